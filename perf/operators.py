@@ -116,7 +116,8 @@ def _activations(g, m, d):
 def _quantized(x):
     """int8 rows and their scales, largest magnitude / 127."""
     amax = x.abs().amax(1, keepdim=True).clamp_min(TINY)
-    return torch.round(x * (127.0 / amax)).to(torch.int8), (amax / 127.0)[:, 0].contiguous()
+    inv = torch.full_like(amax, 127.0) / amax
+    return torch.round(x * inv).to(torch.int8), (amax / 127.0)[:, 0].contiguous()
 
 
 def _lengths(case, which):
