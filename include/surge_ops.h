@@ -3,8 +3,9 @@
  *
  * Each call runs one stage of the encode path on caller-provided device
  * buffers, with the same kernels surge_encode_superbatch launches, so every
- * stage can be checked on its own.  The call is synchronous: it enqueues on
- * `hip_stream` (NULL = null stream) and waits for it before returning.
+ * stage can be checked on its own.  The call is synchronous unless its
+ * comment says otherwise: it enqueues on `hip_stream` (NULL = null stream)
+ * and waits for it before returning.
  * bf16 tensors are passed as uint16_t bit patterns.  Text boundaries are
  * given as host int64 cu_seqlens [n_texts+1] (cu[0] = 0, increasing), checked
  * on the host and copied to the device by the call.  Returns the status
@@ -127,6 +128,118 @@ surge_status surge_op_layernorm(int64_t M, int32_t d, const uint16_t* d_x, const
  * [n_texts, d], 16-byte aligned.  d % 128 == 0, d <= 1024. */
 surge_status surge_op_pool_l2(int64_t n_texts, const int64_t* h_cu_seqlens, int32_t d,
                               const uint16_t* d_x, float* d_out, void* hip_stream);
+
+/*
+ * Operators of models that read the encoder's token states (a reranker, a
+ * pooling head with latent queries, a decoder of answers): the linear layer
+ * in 8-bit integers, the norms around a block, and attention to a text's
+ * states.  Unlike the stages above these calls only enqueue on `hip_stream`:
+ * they do not synchronise, allocate or copy, so they can be captured into a
+ * HIP graph (with buffers, workspace and plan that live as long as the
+ * graph).  Buffers and stream belong to the current device.  A matrix has a
+ * row stride `ld`, in elements, of at most 2^22, and 16-byte aligned rows
+ * (ld a multiple of 8 for bf16, of 16 for int8).  M = 0 rows is a call that
+ * does nothing.
+ */
+
+/*
+ * Rows quantized to int8 with a scale per row (per token of activations, per
+ * output channel of a weight): with a = max(max_k |x[m][k]|, 2^-100),
+ *   q[m][k] = round(x[m][k] * (127 / a)) (ties to even), scale[m] = a / 127.
+ * d_x bf16 [M, K]; d_q int8 [M, K rounded up to a multiple of 128], the
+ * columns from K on set to 0; d_scale fp32 [M].  A row with an infinity or a
+ * NaN gets q = 0 and scale = NaN, which marks every output made from it.
+ * K % 8 == 0, K <= 16384.  d_q must not overlap d_x.
+ */
+surge_status surge_op_quantize_rows(int64_t M, int32_t K, const uint16_t* d_x, int64_t ld_x,
+                                    int8_t* d_q, int64_t ld_q, float* d_scale, void* hip_stream);
+
+/*
+ * Linear layer in 8-bit integers with scales for each token and channel:
+ *   y[m][n] = epi(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n]).
+ * d_x int8 [M, K]; d_x_scale fp32 [M]; d_w int8 [N, K] contiguous (out, in);
+ * d_w_scale, d_bias fp32 [N], 16-byte aligned; epilogue as surge_op_linear (0
+ * bias, 1 exact GELU, 2 + d_res, bf16 [M, N]); d_y bf16 [M, N].  The sum over
+ * k is exact (32-bit integers).  K % 128 == 0, K <= 65536 (pad both operands
+ * with zeros, as surge_op_quantize_rows does); N % 8 == 0, N <= 2^20.  d_y
+ * may be d_res with the same stride; it must not overlap the other inputs.
+ */
+surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d_x, int64_t ld_x,
+                                const float* d_x_scale, const int8_t* d_w, const float* d_w_scale,
+                                const float* d_bias, const uint16_t* d_res, int64_t ld_res,
+                                int32_t epilogue, uint16_t* d_y, int64_t ld_y, void* hip_stream);
+
+/* Norms of surge_op_block_norm over a row v of d features. */
+#define SURGE_NORM_LAYER 0 /* gamma (v - mean) / sqrt(var + eps) + beta, biased variance */
+#define SURGE_NORM_RMS 1   /* gamma v / sqrt(mean of v^2 + eps) */
+
+/*
+ * What lies between two blocks of a model, in one pass over the rows:
+ *   y = res_scale * x + gate * gate_rows * N_post(block)
+ *   z = N_pre(y)
+ * d_x, d_block, d_gate_rows bf16 [M, d]; the gammas, betas and d_gate fp32
+ * [d], 16-byte aligned.  Outputs: d_y bf16 [M, d], the residual stream; d_z
+ * bf16 [M, d], the next block's input; d_zq int8 with d_zq_scale fp32 [M],
+ * the same rows as surge_op_quantize_rows gives them, before a rounding to
+ * bf16 (d_zq has d rounded up to a multiple of 128 columns).  Each output may
+ * be NULL, not all.  z is made from y before its rounding to bf16.
+ * NULL inputs: d_block (y = res_scale * x; then no post norm or gate),
+ * d_post_gamma (no norm after the block), either beta (0; always NULL for
+ * SURGE_NORM_RMS), d_gate, d_gate_rows (1).  d_pre_gamma is needed for z.
+ * d % 8 == 0, d <= 8192; eps in [0, 1].  d_y and d_z may each be d_x, d_block
+ * or d_gate_rows with the same stride (not the same one); otherwise outputs
+ * must not overlap inputs or each other.
+ */
+surge_status surge_op_block_norm(int64_t M, int32_t d, int32_t kind, const uint16_t* d_x,
+                                 int64_t ld_x, const uint16_t* d_block, int64_t ld_block,
+                                 const float* d_post_gamma, const float* d_post_beta,
+                                 const float* d_gate, const uint16_t* d_gate_rows, int64_t ld_gate,
+                                 float res_scale, const float* d_pre_gamma, const float* d_pre_beta,
+                                 float eps, uint16_t* d_y, int64_t ld_y, uint16_t* d_z, int64_t ld_z,
+                                 int8_t* d_zq, int64_t ld_zq, float* d_zq_scale, void* hip_stream);
+
+/*
+ * The work list of cross attention for a batch's lengths, on the current
+ * device.  Sequence i has the queries cu_q[i] .. cu_q[i+1]-1 and the states
+ * cu_kv[i] .. cu_kv[i+1]-1 of its text (host int64 [n_seqs+1], from 0, never
+ * decreasing: either length may be 0).  n_heads query heads share n_kv_heads
+ * key heads in equal groups (head h reads key head h / (n_heads /
+ * n_kv_heads)); d_head is 32, 64 or 128.  The lengths of a text's states stay
+ * what they are over the layers and steps of its reader, so a plan is made
+ * once.  It is not changed by the calls that use it, from any thread or
+ * stream; destroy it after the last of them has finished.  Create and
+ * destroy allocate, copy and free device memory and cannot be captured.
+ */
+typedef struct surge_cross_plan surge_cross_plan;
+surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, const int64_t* h_cu_kv,
+                                     int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                                     surge_cross_plan** out);
+void surge_cross_plan_destroy(surge_cross_plan* plan);
+
+/* Bytes of workspace that a call needs, the units of work it launches and
+ * how many of them hold a part of their rows' keys.  Each pointer may be
+ * NULL. */
+surge_status surge_cross_plan_info(const surge_cross_plan* plan, int64_t* workspace_bytes,
+                                   int64_t* n_units, int64_t* n_parts);
+
+/*
+ * Cross attention: out[t][h] = sum_k p_k v[k] / sum_k p_k over the states k
+ * of t's text, p_k = exp(scale q[t][h] . k[k]); a sequence without states, or
+ * with none left by the mask, gives zeros.
+ * d_q, d_out bf16 [cu_q[n], n_heads d_head]; d_k, d_v bf16 [cu_kv[n],
+ * n_kv_heads d_head] (two column ranges of one projection's output, say, with
+ * its stride); d_key_mask one byte per state, 0 leaves it out (what stands in
+ * its rows of k and v does not matter), or NULL; scale positive and finite.
+ * d_workspace: 16-byte aligned, of at least the plan's bytes (NULL where
+ * that is 0), used until the call's work is done: calls that may run at the
+ * same time, graph replays among them, need one each.  d_out must not
+ * overlap an input.
+ */
+surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16_t* d_q, int64_t ld_q,
+                                      const uint16_t* d_k, int64_t ld_k, const uint16_t* d_v,
+                                      int64_t ld_v, const uint8_t* d_key_mask, float scale,
+                                      void* d_workspace, int64_t workspace_bytes, uint16_t* d_out,
+                                      int64_t ld_out, void* hip_stream);
 
 #ifdef __cplusplus
 }

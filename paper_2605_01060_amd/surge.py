@@ -30,6 +30,9 @@ SURGE_POLICY_LITERAL = 1
 SURGE_WEIGHTS_F32 = 0
 SURGE_WEIGHTS_BF16 = 1
 
+NORM_LAYER = 0
+NORM_RMS = 1
+
 KERNEL_NAMES = ["embed", "qkv", "attn", "oproj", "ln1", "ffn1", "ffn2", "ln2", "pool"]
 
 SEGMENT_DTYPE = np.dtype([("first_text", "<i8"), ("count", "<i8"), ("row_offset", "<i8"),
@@ -99,6 +102,17 @@ _SIGNATURES = {
     "surge_op_attention": ([_I64, _P, _I32, _I32, _P, _P, _P], _I32),
     "surge_op_layernorm": ([_I64, _I32, _P, _P, _P, ctypes.c_float, _P, _P], _I32),
     "surge_op_pool_l2": ([_I64, _P, _I32, _P, _P, _P], _I32),
+    "surge_op_quantize_rows": ([_I64, _I32, _P, _I64, _P, _I64, _P, _P], _I32),
+    "surge_op_linear_i8": ([_I64, _I32, _I32, _P, _I64, _P, _P, _P, _P, _P, _I64, _I32, _P, _I64,
+                            _P], _I32),
+    "surge_op_block_norm": ([_I64, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64,
+                             ctypes.c_float, _P, _P, ctypes.c_float, _P, _I64, _P, _I64, _P, _I64,
+                             _P, _P], _I32),
+    "surge_cross_plan_create": ([_I64, _P, _P, _I32, _I32, _I32, _P], _I32),
+    "surge_cross_plan_destroy": ([_P], None),
+    "surge_cross_plan_info": ([_P, _P, _P, _P], _I32),
+    "surge_op_cross_attention": ([_P, _P, _I64, _P, _I64, _P, _I64, _P, ctypes.c_float, _P, _I64,
+                                  _P, _I64, _P], _I32),
 }
 
 
@@ -375,6 +389,83 @@ def surge_op_pool_l2(cu_seqlens, d, d_x, d_out, stream=None):
     cu, pcu = _host(cu_seqlens, np.int64)
     _check(lib().surge_op_pool_l2(cu.shape[0] - 1, pcu, d, _dev(d_x), _dev(d_out),
                                   _stream(stream)))
+
+
+# Operators of a reader of the encoder's states (asynchronous) ----------------
+
+def surge_op_quantize_rows(M, K, d_x, ld_x, d_q, ld_q, d_scale, stream=None):
+    _check(lib().surge_op_quantize_rows(M, K, _dev(d_x), ld_x, _dev(d_q), ld_q, _dev(d_scale),
+                                        _stream(stream)))
+
+
+def surge_op_linear_i8(M, N, K, d_x, ld_x, d_x_scale, d_w, d_w_scale, d_bias, d_res, ld_res,
+                       epilogue, d_y, ld_y, stream=None):
+    _check(lib().surge_op_linear_i8(M, N, K, _dev(d_x), ld_x, _dev(d_x_scale), _dev(d_w),
+                                    _dev(d_w_scale), _dev(d_bias), _dev(d_res), ld_res, epilogue,
+                                    _dev(d_y), ld_y, _stream(stream)))
+
+
+def surge_op_block_norm(M, d, kind, d_x, ld_x, d_block, ld_block, post_gamma, post_beta, gate,
+                        gate_rows, ld_gate, res_scale, pre_gamma, pre_beta, eps, d_y, ld_y, d_z,
+                        ld_z, d_zq, ld_zq, zq_scale, stream=None):
+    _check(lib().surge_op_block_norm(M, d, kind, _dev(d_x), ld_x, _dev(d_block), ld_block,
+                                     _dev(post_gamma), _dev(post_beta), _dev(gate),
+                                     _dev(gate_rows), ld_gate, res_scale, _dev(pre_gamma),
+                                     _dev(pre_beta), eps, _dev(d_y), ld_y, _dev(d_z), ld_z,
+                                     _dev(d_zq), ld_zq, _dev(zq_scale), _stream(stream)))
+
+
+def surge_cross_plan_create(cu_q, cu_kv, n_heads: int, n_kv_heads: int, d_head: int) -> int:
+    cq, pq = _host(cu_q, np.int64)
+    ck, pk = _host(cu_kv, np.int64)
+    if cq.shape != ck.shape:
+        raise ValueError("cu_q and cu_kv have to be of one length")
+    h = ctypes.c_void_p(0)
+    _check(lib().surge_cross_plan_create(cq.shape[0] - 1, pq, pk, n_heads, n_kv_heads, d_head,
+                                         ctypes.byref(h)))
+    return h.value
+
+
+def surge_cross_plan_destroy(plan: int):
+    lib().surge_cross_plan_destroy(plan)
+
+
+def surge_cross_plan_info(plan: int) -> Tuple[int, int, int]:
+    """Workspace bytes, units of work, and units that hold a part of the keys."""
+    v = [ctypes.c_int64(0) for _ in range(3)]
+    _check(lib().surge_cross_plan_info(plan, *[ctypes.byref(x) for x in v]))
+    return tuple(x.value for x in v)
+
+
+def surge_op_cross_attention(plan, d_q, ld_q, d_k, ld_k, d_v, ld_v, key_mask, scale, workspace,
+                             d_out, ld_out, stream=None):
+    """plan: a CrossPlan.  workspace: a device tensor of at least
+    plan.workspace_bytes bytes (None where that is 0)."""
+    _check(lib().surge_op_cross_attention(plan.handle, _dev(d_q), ld_q, _dev(d_k), ld_k, _dev(d_v),
+                                          ld_v, _dev(key_mask), scale, _dev(workspace),
+                                          0 if workspace is None else workspace.nbytes,
+                                          _dev(d_out), ld_out, _stream(stream)))
+
+
+class CrossPlan:
+    """Owns a surge_cross_plan."""
+
+    handle = 0
+
+    def __init__(self, cu_q, cu_kv, n_heads: int, n_kv_heads: int, d_head: int):
+        self.handle = surge_cross_plan_create(cu_q, cu_kv, n_heads, n_kv_heads, d_head)
+        self.workspace_bytes, self.n_units, self.n_parts = surge_cross_plan_info(self.handle)
+
+    def close(self):
+        if self.handle:
+            surge_cross_plan_destroy(self.handle)
+            self.handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # Convenience: an encoder object over device-resident inputs ----------------
