@@ -46,17 +46,27 @@ __device__ __forceinline__ int kv_copy_chunk(int lane, int copy) {
     return copy_chunk<CPR>(lane, copy);
 }
 
-template <int DH>
-__global__ __launch_bounds__(64) void cross_attention_kernel(CrossAttention a) {
+// WAVES waves of 32 rows against blocks of KB keys that they share in LDS, the
+// next block copied while the current one is on the MFMA units.
+template <int DH, int WAVES, int KB>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void cross_kernel(
+    CrossAttention a, const CrossItem* items) {
   constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8;
-  constexpr int RPC = 64 / CPR, NCP = 32 / RPC, BLK = 32 * CPR;
-  __shared__ u32x4 sK[2][BLK];
-  __shared__ u32x4 sV[2][BLK];
-  const int lane = threadIdx.x, col = lane & 31, half = lane >> 5;
+  constexpr int RPC = 64 / CPR;          // rows that a copy instruction fills
+  constexpr int NCP = KB / RPC / WAVES;  // copies per wave of a block of K or V
+  constexpr int T = KB / 32;             // 32-key tiles of a block
+  constexpr uint32_t ROW = DH * 2, BUF = KB * ROW;  // bytes of an LDS row, of a block
+  constexpr uint64_t FULL = KB == 64 ? ~0ull : 0xffffffffull;
+  static_assert((KB == 32 || KB == 64) && NCP >= 1, "a block is copied by whole instructions");
+  __shared__ __attribute__((aligned(256))) u32x4 sKV[4 * BUF / 16];  // K blocks by parity, then V blocks
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % a.n_kv_heads;
-  const CrossItem item = a.items[blockIdx.x / a.n_kv_heads];
+  const CrossItem item = items[blockIdx.x / a.n_kv_heads];
   const int G = a.group;
-  const int row = min(item.row0 + col, item.rows - 1);
+  const int row0 = item.row0 + wave * 32;
+  const bool active = row0 < item.rows;  // a wave without rows still copies
+  const int row = min(row0 + col, item.rows - 1);
   const int64_t token = (int64_t)item.q_beg + row / G;
   const int head = kvh * G + row % G;
 
@@ -65,108 +75,148 @@ __global__ __launch_bounds__(64) void cross_attention_kernel(CrossAttention a) {
   for (int kk = 0; kk < KSTEPS; ++kk)
     qf[kk] = *reinterpret_cast<const bf16x8*>(a.q + token * a.ld_q + head * DH + (kk * 2 + half) * 8);
 
-  const uint16_t* kb = a.k + (int64_t)item.kv_beg * a.ld_k + kvh * DH;
-  const uint16_t* vb = a.v + (int64_t)item.kv_beg * a.ld_v + kvh * DH;
-  const uint8_t* mask = a.mask ? a.mask + item.kv_beg : nullptr;
-  const uint32_t lk = lds_address(sK[0]), lv = lds_address(sV[0]);
-  auto copy_block = [&](int k0, int b) {
+  const int n_keys = item.k1 - item.k0;
+  const int n = (n_keys + KB - 1) / KB;
+  const uint16_t* kb = a.k + ((int64_t)item.kv_beg + item.k0) * a.ld_k + kvh * DH;
+  const uint16_t* vb = a.v + ((int64_t)item.kv_beg + item.k0) * a.ld_v + kvh * DH;
+  const uint8_t* mask = a.mask ? a.mask + item.kv_beg + item.k0 : nullptr;
+  const uint32_t lds = lds_address(sKV);
+  const uint32_t lcopy = __builtin_amdgcn_readfirstlane(lds + wave * (NCP * 1024));
+  // This wave's copies of block i into buffer i % 2; rows past the unit's
+  // keys are read clamped.
+  auto copy_block = [&](const uint16_t* base, int64_t ld, int i, uint32_t to) {
+    const uint16_t* src = base + (int64_t)i * KB * ld;
 #pragma unroll
     for (int j = 0; j < NCP; ++j) {
-      const int r = min(k0 + j * RPC + lane / CPR, item.k1 - 1);
-      const int c = kv_copy_chunk<CPR>(lane, j) * 8;
-      copy_to_lds16(kb + r * a.ld_k + c, lk + b * (BLK * 16) + j * 1024);
-      copy_to_lds16(vb + r * a.ld_v + c, lv + b * (BLK * 16) + j * 1024);
+      const int jj = wave * NCP + j;
+      const uint32_t r = (uint32_t)min(jj * RPC + lane / CPR, n_keys - 1 - i * KB);
+      copy_to_lds16_at(src, r * (uint32_t)ld * 2u + (uint32_t)kv_copy_chunk<CPR>(lane, jj) * 16u,
+                       lcopy + to + j * 1024);
     }
   };
+  auto copy_kv = [&](int i) {
+    copy_block(kb, a.ld_k, i, (i & 1) * BUF);
+    copy_block(vb, a.ld_v, i, (2 + (i & 1)) * BUF);
+  };
+  // Key KB i + lane (% 32 of a 32-key block) is there and not masked.
+  auto key_on = [&](int i) {
+    const int key = i * KB + (lane & (KB - 1));
+    bool on = key < n_keys;
+    if (mask && on) on = mask[key] != 0;
+    return on;
+  };
 
-  float m_run = -INFINITY, l_run = 0.0f;
+  // LDS addresses.  K: chunk 2 kk + half of row col; the swizzle is an
+  // exclusive or, so step kk is one of the address.  V: 4 features of key 16 c
+  // + 8 h + tr_key from dt 32 + tr_feat on; the swizzle of h and dt likewise.
+  const int tr_key = 4 * half + ((lane & 15) >> 2);
+  const int tr_feat = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  uint32_t ka = lds + (uint32_t)kv_slot<CPR>(col, half) * 16u;
+  uint32_t va = lds + 2 * BUF + (uint32_t)kv_slot<CPR>(tr_key, tr_feat >> 3) * 16u + (tr_feat & 7) * 2u;
+  constexpr uint32_t H_SWZ = CPR == 16 ? 128 : 16;  // of 8 keys further on
+  auto k_fragment = [&](int t, int kk) {
+    return __builtin_bit_cast(
+        bf16x8, *(const __attribute__((address_space(3))) u32x4*)((ka ^ kk * 32) + t * 32 * ROW));
+  };
+  auto v_fragment = [&](int c, int dt) {
+    bf16x4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      v[h] = __builtin_bit_cast(
+          bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(
+                      (va ^ (dt * 64 ^ h * H_SWZ)) + (16 * c + 8 * h) * ROW)));
+    return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  float m_ref = -INFINITY, l_run = 0.0f;
   f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
-  const int tr_key = 4 * half + ((lane & 15) >> 2);
-  const int tr_feat = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 
-  int b = 0;
-  if (item.k0 < item.k1) copy_block(item.k0, 0);
-  for (int k0 = item.k0; k0 < item.k1; k0 += 32, b ^= 1) {
-    // Key k0 + col is there and not masked, as bit col of `keys`.
-    const int kc = k0 + col;
-    bool on = kc < item.k1;
-    if (mask && on) on = mask[kc] != 0;
-    const uint32_t keys = (uint32_t)__ballot(on);
+  bool on = false;
+  if (n > 0) {
+    copy_kv(0);
+    on = key_on(0);
+  }
+  for (int i = 0; i < n; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (k0 + 32 < item.k1) copy_block(k0 + 32, b ^ 1);
-    if (keys == 0) continue;
-    if (keys != ~0u) {
-      // What stands in the V rows of absent keys must not reach the products,
-      // where a NaN or infinity times 0 would.
+    const uint64_t keys = __ballot(on) & FULL;
+    if (keys != FULL) {
+      // What stands in the V rows of absent keys must not reach the products.
 #pragma unroll
       for (int j = 0; j < NCP; ++j)
-        if (!(keys >> (j * RPC + lane / CPR) & 1)) sV[b][j * 64 + lane] = u32x4{0u, 0u, 0u, 0u};
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (!(keys >> ((wave * NCP + j) * RPC + lane / CPR) & 1))
+          sKV[(2 + (i & 1)) * (BUF / 16) + (wave * NCP + j) * 64 + lane] = u32x4{0u, 0u, 0u, 0u};
     }
-    f32x16 s;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
-#pragma unroll
-    for (int kk = 0; kk < KSTEPS; ++kk)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          __builtin_bit_cast(bf16x8, sK[b][kv_slot<CPR>(col, kk * 2 + half)]), qf[kk], s, 0, 0, 0);
-    if (keys != ~0u) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!(keys >> (8 * (r >> 2) + 4 * half + (r & 3)) & 1)) s[r] = -INFINITY;
+    __syncthreads();  // the block is there, the other one read out
+    if (i + 1 < n) {
+      copy_kv(i + 1);
+      on = key_on(i + 1);
     }
-    float mloc = s[0];
+    if (active && keys) {
+      f32x16 s[T];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mloc = fmaxf(mloc, s[r]);
-    mloc = fmaxf(mloc, __shfl_xor(mloc, 32, 64));
-    const float m_new = fmaxf(m_run, mloc * a.scale_log2);
-    float psum = 0.0f;
+      for (int t = 0; t < T; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m_new));
-      psum += s[r];
-    }
-    psum += __shfl_xor(psum, 32, 64);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-    l_run = fmaf(l_run, alpha, psum);
-    m_run = m_new;
+        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+      for (int kk = 0; kk < KSTEPS; ++kk)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
-    bf16x8 pb[2];
+        for (int t = 0; t < T; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
+      if (keys != FULL) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+        for (int t = 0; t < T; ++t)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) pb[c][j] = (__bf16)s[8 * c + j];
-    const char* vbytes = reinterpret_cast<const char*>(sV[b]);
+          for (int r = 0; r < 16; ++r)
+            if (!(keys >> (32 * t + 8 * (r >> 2) + 4 * half + (r & 3)) & 1)) s[t][r] = -INFINITY;
+      }
+      float mloc = s[0][0];
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const int feat = dt * 32 + tr_feat;
+      for (int r = 1; r < 16 * T; ++r) mloc = fmaxf(mloc, s[r >> 4][r & 15]);
+      mloc = fmaxf(mloc, __shfl_xor(mloc, 32, 64)) * a.scale_log2;
+      // The reference of the exponentials follows the maximum only where that
+      // has grown by more than 2^8: the probabilities stay below 2^8.
+      if (__any(mloc > m_ref + 8.0f)) {
+        const float m_new = fmaxf(m_ref, mloc);
+        const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+        m_ref = m_new;
+        l_run *= alpha;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        bf16x4 v2[2];
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const char* pa = vbytes + kv_slot<CPR>(16 * c + 8 * i + tr_key, feat >> 3) * 16 + (feat & 7) * 2;
-          v2[i] = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                 (__attribute__((address_space(3))) i16x4*)pa));
+          for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      }
+#pragma unroll
+      for (int c = 0; c < 2 * T; ++c) {
+        bf16x8 pb;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][8 * (c & 1) + r], a.scale_log2, -m_ref));
+          l_run += p;
+          pb[r] = (__bf16)p;
         }
-        const bf16x8 va = __builtin_shufflevector(v2[0], v2[1], 0, 1, 2, 3, 4, 5, 6, 7);
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[c], o[dt], 0, 0, 0);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(c, dt), pb, o[dt], 0, 0, 0);
       }
     }
+    const uint32_t other = i & 1 ? 0u - BUF : BUF;
+    ka += other;
+    va += other;
   }
+  l_run += __shfl_xor(l_run, 32, 64);
 
-  // Register r of tile dt: feature dt 32 + 8 (r / 4) + 4 half + r % 4.
-  if (item.row0 + col >= item.rows) return;
+  // Register r of tile dt: feature dt 32 + 8 (r / 4) + 4 half + r % 4 of row col.
   if (item.part < 0) {
+    // Staged in LDS, so that whole rows are stored (8 bytes a lane from the
+    // registers are four times as many requests).
+    __syncthreads();  // every wave has read its last block
+    if (!active) return;
     const float inv = l_run > 0.0f ? 1.0f / l_run : 0.0f;
-    uint16_t* out = a.out + token * a.ld_out + head * DH;
+    u32x4* stage = sKV + wave * (32 * CPR);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -174,12 +224,23 @@ __global__ __launch_bounds__(64) void cross_attention_kernel(CrossAttention a) {
         uint2 w;
         w.x = pack_bf16x2(o[dt][4 * g] * inv, o[dt][4 * g + 1] * inv);
         w.y = pack_bf16x2(o[dt][4 * g + 2] * inv, o[dt][4 * g + 3] * inv);
-        *reinterpret_cast<uint2*>(out + dt * 32 + g * 8 + half * 4) = w;
+        reinterpret_cast<uint2*>(stage + kv_slot<CPR>(col, dt * 4 + g))[half] = w;
       }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < CPR / 2; ++j) {
+      const int r = row0 + j * RPC + lane / CPR;
+      const u32x4 w = stage[j * 64 + lane];
+      if (r < item.rows) {
+        uint16_t* to = a.out + ((int64_t)item.q_beg + r / G) * a.ld_out + (kvh * G + r % G) * DH;
+        __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(to + kv_copy_chunk<CPR>(lane, j) * 8));
+      }
+    }
     return;
   }
-  const int64_t slot = ((int64_t)item.part * a.n_kv_heads + kvh) * 32 + col;
-  if (half == 0) a.part_ml[slot] = make_float2(m_run, l_run);
+  if (row0 + col >= item.rows) return;
+  const int64_t slot = ((int64_t)(item.part + wave) * a.n_kv_heads + kvh) * 32 + col;
+  if (half == 0) a.part_ml[slot] = make_float2(m_ref, l_run);
   float* po = a.part_o + slot * DH;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -189,60 +250,110 @@ __global__ __launch_bounds__(64) void cross_attention_kernel(CrossAttention a) {
           make_float4(o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]);
 }
 
-// Joins the parts of one row: a wave per (row, key head), in key order.
-template <int DH>
-__global__ __launch_bounds__(64) void cross_join_kernel(CrossAttention a) {
-  const int kvh = blockIdx.x % a.n_kv_heads;
-  const int unit = blockIdx.x / a.n_kv_heads;
-  const CrossJoin j = a.joins[unit / 32];
-  const int r = unit % 32;
-  if (r >= j.rows) return;
-  const int lane = threadIdx.x;
-  float m = -INFINITY;
-  for (int p = 0; p < j.parts; ++p)
-    m = fmaxf(m, a.part_ml[((int64_t)(j.part0 + p) * a.n_kv_heads + kvh) * 32 + r].x);
+// Joins the parts of a row of one key head in WAVES waves: wave w takes parts
+// w, w + WAVES, ..., BATCH loads in flight, and the waves are added in order.
+// A workgroup has ROWS rows.
+template <int DH, int WAVES, int ROWS, int BATCH>
+__global__ __launch_bounds__(64 * WAVES * ROWS) void cross_join_kernel(CrossAttention a) {
   constexpr int PER = DH < 64 ? 1 : DH / 64;
+  static_assert(WAVES == 1 || ROWS == 1, "waves that meet have one row");
+  __shared__ float sm[WAVES], so[WAVES][DH + 1];
+  const int lane = threadIdx.x & 63;
+  const int wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+  const int first = blockIdx.x / a.n_kv_heads * ROWS;
+  const int kvh = blockIdx.x % a.n_kv_heads;
+  const CrossJoin j = a.joins[first / 32];
+  const int r = first % 32 + (WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+  if (r >= j.rows) return;
+  auto slot = [&](int p) {
+    return ((int64_t)(j.part0 + p * j.stride) * a.n_kv_heads + kvh) * 32 + r;
+  };
+  float m = -INFINITY;
+  for (int p = wave * 64 + lane; p < j.parts; p += 64 * WAVES) m = fmaxf(m, a.part_ml[slot(p)].x);
+  m = wave_max(m);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) sm[wave] = m;
+    __syncthreads();
+    m = sm[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w]);
+  }
   float l = 0.0f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-  if (m > -INFINITY)
-    for (int p = 0; p < j.parts; ++p) {
-      const int64_t slot = ((int64_t)(j.part0 + p) * a.n_kv_heads + kvh) * 32 + r;
-      const float2 ml = a.part_ml[slot];
-      const float f = __builtin_amdgcn_exp2f(ml.x - m);
-      l = fmaf(f, ml.y, l);
+  // Without any key in the row (m = -inf) every part is zeros: nothing to add.
+  for (int p0 = wave; p0 < j.parts && m > -INFINITY; p0 += WAVES * BATCH) {
+    float2 ml[BATCH];
+    float v[BATCH][PER];
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      const int64_t s = slot(min(p0 + q * WAVES, j.parts - 1));
+      ml[q] = a.part_ml[s];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) v[q][i] = lane < DH ? a.part_o[s * DH + lane * PER + i] : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      const float f = p0 + q * WAVES < j.parts ? __builtin_amdgcn_exp2f(ml[q].x - m) : 0.0f;
+      l = fmaf(f, ml[q].y, l);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) o[i] = fmaf(f, v[q][i], o[i]);
+    }
+  }
+  if constexpr (WAVES > 1) {
+    if (lane == 0) so[wave][DH] = l;
+    if (lane < DH)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) so[wave][lane * PER + i] = o[i];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      l += so[w][DH];
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        if (lane + 64 * i < DH) o[i] = fmaf(f, a.part_o[slot * DH + lane + 64 * i], o[i]);
+        if (lane < DH) o[i] += so[w][lane * PER + i];
     }
+  }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   const int row = j.row0 + r;
   uint16_t* out = a.out + ((int64_t)j.q_beg + row / a.group) * a.ld_out + (kvh * a.group + row % a.group) * DH;
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (lane + 64 * i < DH) out[lane + 64 * i] = (uint16_t)(pack_bf16x2(o[i] * inv, 0.0f) & 0xffffu);
+  if constexpr (PER == 2)
+    reinterpret_cast<uint32_t*>(out)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
+  else if (lane < DH)
+    out[lane] = (uint16_t)(pack_bf16x2(o[0] * inv, 0.0f) & 0xffffu);
+}
+
+template <int DH>
+hipError_t launch(const CrossAttention& a, hipStream_t stream) {
+  const unsigned h = (unsigned)a.n_kv_heads;
+  const CrossItem* items = a.items;
+#define SURGE_LAUNCH(CLASS, WAVES, KB)                                                            \
+  if (a.n_items[CLASS] > 0) {                                                                     \
+    hipLaunchKernelGGL((cross_kernel<DH, WAVES, KB>), dim3(a.n_items[CLASS] * h), dim3(64 * WAVES), \
+                       0, stream, a, items);                                                      \
+    items += a.n_items[CLASS];                                                                    \
+  }
+  SURGE_LAUNCH(0, 4, 64)
+  SURGE_LAUNCH(1, 2, 32)
+  SURGE_LAUNCH(2, 1, 32)
+#undef SURGE_LAUNCH
+  const unsigned rows = (unsigned)a.n_joins * 32;
+  if (a.n_joins > 0 && a.max_parts > 64)
+    hipLaunchKernelGGL((cross_join_kernel<DH, 16, 1, 8>), dim3(rows * h), dim3(1024), 0, stream, a);
+  else if (a.n_joins > 0 && a.max_parts > 8)
+    hipLaunchKernelGGL((cross_join_kernel<DH, 4, 1, 8>), dim3(rows * h), dim3(256), 0, stream, a);
+  else if (a.n_joins > 0)
+    hipLaunchKernelGGL((cross_join_kernel<DH, 1, 4, 4>), dim3(rows / 4 * h), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cross_attention(const CrossAttention& a, int d_head, int n_items, int n_joins,
-                                  hipStream_t stream) {
-  if (n_items <= 0) return hipSuccess;
-  const dim3 grid((unsigned)((int64_t)n_items * a.n_kv_heads));
-  const dim3 join((unsigned)((int64_t)n_joins * 32 * a.n_kv_heads));
-#define SURGE_LAUNCH(DH)                                                                     \
-  do {                                                                                       \
-    hipLaunchKernelGGL((cross_attention_kernel<DH>), grid, dim3(64), 0, stream, a);          \
-    if (n_joins > 0) hipLaunchKernelGGL((cross_join_kernel<DH>), join, dim3(64), 0, stream, a); \
-  } while (0)
-  if (d_head == 32)
-    SURGE_LAUNCH(32);
-  else if (d_head == 64)
-    SURGE_LAUNCH(64);
-  else
-    SURGE_LAUNCH(128);
-#undef SURGE_LAUNCH
-  return hipGetLastError();
+hipError_t launch_cross_attention(const CrossAttention& a, int d_head, hipStream_t stream) {
+  if (d_head == 32) return launch<32>(a, stream);
+  if (d_head == 64) return launch<64>(a, stream);
+  return launch<128>(a, stream);
 }
 
 }  // namespace surge

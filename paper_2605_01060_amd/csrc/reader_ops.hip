@@ -25,9 +25,9 @@ struct surge_cross_plan {
   int device = 0;
   int n_kv_heads = 0, group = 0, d_head = 0;
   int64_t q_tokens = 0, kv_tokens = 0;
-  int n_items = 0, n_joins = 0;
+  int n_items[CROSS_CLASSES] = {}, n_units = 0, n_joins = 0, max_parts = 0;
   int64_t n_parts = 0;
-  void* lists = nullptr;  // device: the items, then the joins
+  void* lists = nullptr;  // device: the items of each class, then the joins
 };
 
 namespace {
@@ -203,9 +203,10 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     CrossList list;
     int n_cus = 0;
     HIP_TRY(resolve_cus(&n_cus));
-    build_cross_list(n_seqs, h_cu_q, h_cu_kv, n_kv_heads, group, n_cus, &list);
-    const int64_t most = std::max<int64_t>((int64_t)list.items.size(), 32 * (int64_t)list.joins.size());
-    if (most * n_kv_heads > (int64_t)INT32_MAX)
+    build_cross_list(n_seqs, h_cu_q, h_cu_kv, n_kv_heads, group, d_head, n_cus, &list);
+    int64_t items = 0;
+    for (const auto& v : list.items) items += (int64_t)v.size();
+    if (std::max(items, 32 * (int64_t)list.joins.size()) * n_kv_heads > (int64_t)INT32_MAX)
       return fail(SURGE_ERR_CAPACITY, "too many units of 32 rows");
     surge_cross_plan* p = new surge_cross_plan;
     p->n_kv_heads = n_kv_heads;
@@ -213,15 +214,21 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     p->d_head = d_head;
     p->q_tokens = h_cu_q[n_seqs];
     p->kv_tokens = h_cu_kv[n_seqs];
-    p->n_items = (int)list.items.size();
+    for (int c = 0; c < CROSS_CLASSES; ++c) p->n_items[c] = (int)list.items[c].size();
+    p->n_units = (int)items;
     p->n_joins = (int)list.joins.size();
+    p->max_parts = list.max_parts;
     p->n_parts = list.n_parts;
-    const size_t a = list.items.size() * sizeof(CrossItem), b = list.joins.size() * sizeof(CrossJoin);
+    const size_t bytes = items * sizeof(CrossItem) + list.joins.size() * sizeof(CrossJoin);
     hipError_t e = hipGetDevice(&p->device);
-    if (e == hipSuccess && a + b > 0) e = hipMalloc(&p->lists, a + b);
-    if (e == hipSuccess && a > 0) e = hipMemcpy(p->lists, list.items.data(), a, hipMemcpyHostToDevice);
-    if (e == hipSuccess && b > 0)
-      e = hipMemcpy((char*)p->lists + a, list.joins.data(), b, hipMemcpyHostToDevice);
+    if (e == hipSuccess && bytes > 0) e = hipMalloc(&p->lists, bytes);
+    char* at = (char*)p->lists;
+    auto upload = [&](const void* from, size_t n) {
+      if (e == hipSuccess && n > 0) e = hipMemcpy(at, from, n, hipMemcpyHostToDevice);
+      at += n;
+    };
+    for (const auto& v : list.items) upload(v.data(), v.size() * sizeof(CrossItem));
+    upload(list.joins.data(), list.joins.size() * sizeof(CrossJoin));
     if (e != hipSuccess) {
       surge_cross_plan_destroy(p);
       return fail(e == hipErrorOutOfMemory ? SURGE_ERR_OUT_OF_MEMORY : SURGE_ERR_DEVICE,
@@ -251,7 +258,7 @@ surge_status surge_cross_plan_info(const surge_cross_plan* plan, int64_t* bytes,
   clear_error();
   if (!plan) return fail(SURGE_ERR_INVALID_ARGUMENT, "plan is NULL");
   if (bytes) *bytes = workspace_bytes(plan);
-  if (n_units) *n_units = (int64_t)plan->n_items * plan->n_kv_heads;
+  if (n_units) *n_units = (int64_t)plan->n_units * plan->n_kv_heads;
   if (n_parts) *n_parts = plan->n_parts * plan->n_kv_heads;
   return SURGE_OK;
 }
@@ -265,7 +272,7 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
   if (!plan) return fail(SURGE_ERR_INVALID_ARGUMENT, "plan is NULL");
   if (!(scale > 0.0f) || !isfinite(scale))
     return fail(SURGE_ERR_INVALID_ARGUMENT, "scale=%g must be positive and finite", (double)scale);
-  if (plan->n_items == 0) return SURGE_OK;
+  if (plan->n_units == 0) return SURGE_OK;
   const int64_t kv_cols = (int64_t)plan->n_kv_heads * plan->d_head;
   const int64_t cols = kv_cols * plan->group;
   CHECK(check_matrix("q", d_q, cols, ld_q, 8));
@@ -300,13 +307,15 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
   a.n_kv_heads = plan->n_kv_heads;
   a.group = plan->group;
   a.items = (const CrossItem*)plan->lists;
-  a.joins = (const CrossJoin*)(a.items + plan->n_items);
+  std::copy(plan->n_items, plan->n_items + CROSS_CLASSES, a.n_items);
+  a.joins = (const CrossJoin*)(a.items + plan->n_units);
+  a.n_joins = plan->n_joins;
+  a.max_parts = plan->max_parts;
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)((float*)d_workspace + part_rows(plan) * plan->d_head);
   a.out = d_out;
   a.ld_out = ld_out;
-  HIP_TRY(launch_cross_attention(a, plan->d_head, plan->n_items, plan->n_joins,
-                                 (hipStream_t)hip_stream));
+  HIP_TRY(launch_cross_attention(a, plan->d_head, (hipStream_t)hip_stream));
   return SURGE_OK;
 }
 
