@@ -169,6 +169,14 @@ surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d
                                 const float* d_bias, const uint16_t* d_res, int64_t ld_res,
                                 int32_t epilogue, uint16_t* d_y, int64_t ld_y, void* hip_stream);
 
+/*
+ * The tile that the layer's launch takes for an [M, N] output of K inputs on a
+ * device of n_cus compute units, rows << 16 | channels (host-only; 0 for
+ * shapes that the layer refuses).  Where 256-wide tiles leave some of N over,
+ * the rest takes a launch of its own.  Every tile gives the same bits.
+ */
+int32_t surge_op_linear_i8_tile(int64_t M, int32_t N, int32_t K, int32_t n_cus);
+
 /* Norms of surge_op_block_norm over a row v of d features. */
 #define SURGE_NORM_LAYER 0 /* gamma (v - mean) / sqrt(var + eps) + beta, biased variance */
 #define SURGE_NORM_RMS 1   /* gamma v / sqrt(mean of v^2 + eps) */

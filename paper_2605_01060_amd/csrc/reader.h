@@ -50,5 +50,7 @@ struct LinearI8 {
 };
 hipError_t launch_linear_i8(int64_t M, int N, int K, int epi, const LinearI8& a, int n_cus,
                             hipStream_t stream);
+// The tile of its first (or only) launch, rows << 16 | channels.
+int linear_i8_tile(int64_t M, int N, int K, int n_cus);
 
 }  // namespace surge

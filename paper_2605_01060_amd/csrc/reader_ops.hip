@@ -124,7 +124,7 @@ surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d
   CHECK(check_vector("w", d_w, true));
   CHECK(check_vector("w_scale", d_w_scale, true));
   CHECK(check_vector("bias", d_bias, true));
-  if ((M + 31) / 32 * ((N + 31) / 32) > (int64_t)INT32_MAX)
+  if ((M + 15) / 16 * ((N + 15) / 16) > (int64_t)INT32_MAX)
     return fail(SURGE_ERR_CAPACITY, "M=%lld, N=%d: too many tiles", (long long)M, N);
   int n_cus = 0;
   HIP_TRY(resolve_cus(&n_cus));
@@ -132,6 +132,13 @@ surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d
                       d_res, ld_res, d_y,  ld_y};
   HIP_TRY(launch_linear_i8(M, N, K, epilogue, a, n_cus, (hipStream_t)hip_stream));
   return SURGE_OK;
+}
+
+int32_t surge_op_linear_i8_tile(int64_t M, int32_t N, int32_t K, int32_t n_cus) {
+  if (M < 1 || M > (int64_t)INT32_MAX || N < 8 || N % 8 || N > 1 << 20 || K < 128 || K % 128 ||
+      K > 65536 || n_cus < 1)
+    return 0;
+  return linear_i8_tile(M, N, K, n_cus);
 }
 
 surge_status surge_op_block_norm(int64_t M, int32_t d, int32_t kind, const uint16_t* d_x,

@@ -105,6 +105,7 @@ _SIGNATURES = {
     "surge_op_quantize_rows": ([_I64, _I32, _P, _I64, _P, _I64, _P, _P], _I32),
     "surge_op_linear_i8": ([_I64, _I32, _I32, _P, _I64, _P, _P, _P, _P, _P, _I64, _I32, _P, _I64,
                             _P], _I32),
+    "surge_op_linear_i8_tile": ([_I64, _I32, _I32, _I32], _I32),
     "surge_op_block_norm": ([_I64, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64,
                              ctypes.c_float, _P, _P, ctypes.c_float, _P, _I64, _P, _I64, _P, _I64,
                              _P, _P], _I32),
@@ -403,6 +404,12 @@ def surge_op_linear_i8(M, N, K, d_x, ld_x, d_x_scale, d_w, d_w_scale, d_bias, d_
     _check(lib().surge_op_linear_i8(M, N, K, _dev(d_x), ld_x, _dev(d_x_scale), _dev(d_w),
                                     _dev(d_w_scale), _dev(d_bias), _dev(d_res), ld_res, epilogue,
                                     _dev(d_y), ld_y, _stream(stream)))
+
+
+def surge_op_linear_i8_tile(M: int, N: int, K: int, n_cus: int = 256):
+    """(rows, channels) of the tile that an [M, N] int8 layer's launch takes."""
+    tile = int(lib().surge_op_linear_i8_tile(M, N, K, n_cus))
+    return tile >> 16, tile & 0xffff
 
 
 def surge_op_block_norm(M, d, kind, d_x, ld_x, d_block, ld_block, post_gamma, post_beta, gate,

@@ -148,6 +148,39 @@ def test_linear_i8(M, N, K, epi):
     assert (big[:M, N:] == 7).all() and (big[M] == 7).all()
 
 
+# (rows, channels) of the tile, and shapes that take it on 256 compute units;
+# the last two leave channels over for a second launch.
+TILES = [((16, 16), 33, 1000, 768), ((64, 64), 300, 1000, 384), ((64, 128), 777, 1536, 384),
+         ((128, 128), 4100, 1032, 256), ((192, 256), 13_579, 768, 768), ((256, 256), 6000, 2304, 768),
+         ((192, 256), 20_000, 1032, 1024), ((256, 256), 30_000, 1288, 2048)]
+
+
+@pytest.mark.parametrize("tile,M,N,K", TILES)
+@pytest.mark.parametrize("epi", [0, 1, 2])
+def test_linear_i8_tiles(tile, M, N, K, epi):
+    """Each kernel, and the bits of its rows in calls of a few rows."""
+    torch = torch_cuda()
+    assert S.surge_op_linear_i8_tile(M, N, K) == tile
+    p = linear_inputs(M, N, K, M + epi)
+    stream = torch.cuda.current_stream()
+
+    def call(rows):
+        y = torch.empty(len(rows), N, dtype=torch.bfloat16, device="cuda")
+        res = p["res"][rows].contiguous() if epi == 2 else None
+        S.surge_op_linear_i8(len(rows), N, K, p["x"][rows].contiguous(), K,
+                             p["xs"][rows].contiguous(), p["w"], p["ws"], p["bias"], res, N, epi, y, N,
+                             stream)
+        return y
+
+    y = call(torch.arange(M).cuda())
+    rows = torch.unique(torch.cat([torch.arange(0, M, 97), torch.tensor([1, 255, 256, M - 2, M - 1])])).cuda()
+    rows = rows[rows < M]
+    ref, tol = linear_reference(p, epi, rows)
+    within(y[rows], ref, tol)
+    few = rows[:: max(1, len(rows) // 7)][:7]
+    assert torch.equal(call(few), y[few])
+
+
 def test_linear_i8_sums_exactly():
     """Sums that need all of 31 bits, the extreme values of int8 among them."""
     torch = torch_cuda()

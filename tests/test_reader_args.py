@@ -108,3 +108,9 @@ def test_no_rows_is_a_call_that_does_nothing():
     S.surge_op_quantize_rows(0, 128, 0, 0, 0, 0, 0)
     S.surge_op_linear_i8(0, 8, 128, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
     S.surge_op_block_norm(**{**NORM, "M": 0})
+
+
+def test_linear_i8_tile_of_refused_shapes():
+    for shape in ((0, 8, 128), (1, 4, 128), (1, 8, 64), (1 << 31, 8, 128), (1, 8, 131072)):
+        assert S.surge_op_linear_i8_tile(*shape) == (0, 0)
+    assert S.surge_op_linear_i8_tile(1, 8, 128, 0) == (0, 0)
