@@ -2,8 +2,8 @@
 // scale per token, and the norms after a block and before the next one fused
 // with the gate, the residual scale and the quantizer.
 //
-// A row is held in registers by LANES lanes (a part of a wave, a wave, or the
-// four waves of a workgroup), CH chunks of 8 features a lane, chunk c = j
+// A row is held in registers by LANES lanes (16 or 32 of a wave, a wave, or
+// the four or eight waves of a workgroup), CH chunks of 8 features a lane, chunk c = j
 // LANES + lane: every load and store of a row is contiguous.  So each input
 // is read once, the mean and the variance are two passes over registers (no
 // E[v^2] - mean^2 cancellation), and all sums are fp32.
@@ -17,25 +17,47 @@
 namespace surge {
 namespace {
 
-constexpr int BLOCK = 256;
+// Threads of a workgroup: of several rows, or the lanes of one.
+constexpr int block_of(int lanes) { return lanes > 256 ? lanes : 256; }
 
 enum Reduce { SUM, MAX };
 
-// Sum or maximum over the LANES lanes of a row.  LANES = 256: the workgroup,
-// through `lds` (4 floats, one use per call between two barriers).
+template <Reduce OP>
+__device__ __forceinline__ float combine(float a, float b) {
+  return OP == SUM ? a + b : fmaxf(a, b);
+}
+
+// v combined with its value in another lane of the same 16 (a DPP control).
+template <Reduce OP, int CTRL>
+__device__ __forceinline__ float with_lane(float v) {
+  return combine<OP>(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)));
+}
+
+// Sum or maximum over the LANES lanes of a row, all lanes of the wave active.
+// Exchanges in registers: a reduction over a wave is six of them, where one
+// through LDS is six LDS latencies.  LANES > 64: the workgroup, through one
+// of two LDS slots by turns, so that one barrier a call is enough.
 template <int LANES, Reduce OP>
-__device__ __forceinline__ float row_reduce(float v, float* lds) {
-#pragma unroll
-  for (int o = (LANES < 64 ? LANES : 64) / 2; o >= 1; o >>= 1) {
-    const float w = __shfl_xor(v, o, 64);
-    v = OP == SUM ? v + w : fmaxf(v, w);
+__device__ __forceinline__ float row_reduce(float v, float (&lds)[2][16], int& turn) {
+  v = with_lane<OP, 0xB1>(v);   // lane ^ 1
+  v = with_lane<OP, 0x4E>(v);   // lane ^ 2
+  v = with_lane<OP, 0x141>(v);  // 7 - lane of 8
+  v = with_lane<OP, 0x140>(v);  // 15 - lane of 16
+  if constexpr (LANES >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = combine<OP>(__uint_as_float(r[0]), __uint_as_float(r[1]));
   }
-  if constexpr (LANES == 256) {
-    __syncthreads();  // the previous use has been read
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  if constexpr (LANES >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = combine<OP>(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) lds[turn][threadIdx.x >> 6] = v;
     __syncthreads();
-    v = OP == SUM ? (lds[0] + lds[1]) + (lds[2] + lds[3])
-                  : fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    v = lds[turn][0];
+#pragma unroll
+    for (int w = 1; w < LANES / 64; ++w) v = combine<OP>(v, lds[turn][w]);
+    turn ^= 1;
   }
   return v;
 }
@@ -50,6 +72,16 @@ struct RowScale {
 __device__ __forceinline__ RowScale row_scale(float amax) {
   const float a = fmaxf(amax, 0x1p-100f);
   return {127.0f / a, a / 127.0f};
+}
+
+// Rows are touched once: loads and stores that leave the caches to others (an
+// L2 that keeps the outputs writes them back beside the next reads: 200,003
+// rows of 1024 with gate rows 428 -> 340 us, of 768 418 -> 302).
+__device__ __forceinline__ uint4 load16(const uint16_t* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+}
+__device__ __forceinline__ void store16(uint16_t* p, uint4 v) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
 }
 
 // The largest magnitude of 8 values, infinity where one is not finite (fmaxf
@@ -68,52 +100,96 @@ __device__ __forceinline__ uint2 quantize8(const float* f, float inv) {
   return {w[0], w[1]};
 }
 
-// What surge.h calls a row that cannot be quantized: zeros under a NaN scale.
+// A row that cannot be quantized: zeros under a NaN scale.
 __device__ __forceinline__ RowScale poisoned() { return {0.0f, NAN}; }
 
-template <int LANES, int CH>
-__global__ __launch_bounds__(BLOCK) void quantize_rows_kernel(int64_t M, int K,
-                                                              const uint16_t* x, int64_t ld_x,
-                                                              int8_t* q, int64_t ld_q,
-                                                              float* scale) {
-  constexpr int ROWS = BLOCK / LANES;
-  __shared__ float lds[4];
-  const int lane = threadIdx.x % LANES;
-  const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (m >= M) return;  // LANES = 256: the whole workgroup
-  const int chunks = K / 8, padded = (K + 127) / 128 * 16;
-  const uint16_t* xr = x + m * ld_x;
-  uint4 raw[CH];
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int c = j * LANES + lane;
-    raw[j] = c < chunks ? *reinterpret_cast<const uint4*>(xr + 8 * c) : uint4{0u, 0u, 0u, 0u};
-  }
+// Quantizes a row of fp32 values, chunk(j, f) giving its chunks.
+template <int LANES, int CH, class Chunk>
+__device__ __forceinline__ void store_quantized(Chunk chunk, int lane, int padded, bool store, int8_t* q,
+                                                float* scale, float (&lds)[2][16], int& turn) {
   float amax = 0.0f, f[8];
 #pragma unroll
   for (int j = 0; j < CH; ++j) {
-    unpack8(raw[j], f);
+    chunk(j, f);
     amax = amax8(f, amax);
   }
-  amax = row_reduce<LANES, MAX>(amax, lds);
+  amax = row_reduce<LANES, MAX>(amax, lds, turn);
   const bool bad = amax == INFINITY;
   const RowScale s = bad ? poisoned() : row_scale(amax);
 #pragma unroll
   for (int j = 0; j < CH; ++j) {
     const int c = j * LANES + lane;
-    unpack8(raw[j], f);
-    if (c < padded)
-      *reinterpret_cast<uint2*>(q + m * ld_q + 8 * c) = bad ? uint2{0u, 0u} : quantize8(f, s.inv);
+    chunk(j, f);
+    if (store && c < padded)
+      *reinterpret_cast<uint2*>(q + 8 * c) = bad ? uint2{0u, 0u} : quantize8(f, s.inv);
   }
-  if (lane == 0) scale[m] = s.scale;
+  if (store && lane == 0) *scale = s.scale;
 }
 
-// v <- the row's norm of v.  Chunks past the row hold 0 and stay out of the
-// variance.
+template <int LANES, int CH>
+__global__ __launch_bounds__(block_of(LANES)) void quantize_rows_kernel(int64_t M, int K,
+                                                              const uint16_t* x, int64_t ld_x,
+                                                              int8_t* q, int64_t ld_q,
+                                                              float* scale) {
+  constexpr int ROWS = block_of(LANES) / LANES;
+  __shared__ float lds[2][16];
+  int turn = 0;
+  const int lane = threadIdx.x % LANES;
+  const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  const int chunks = K / 8;
+  const uint16_t* xr = x + min(m, M - 1) * ld_x;
+  uint4 raw[CH];
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    const int c = j * LANES + lane;
+    raw[j] = c < chunks ? load16(xr + 8 * c) : uint4{0u, 0u, 0u, 0u};
+  }
+  store_quantized<LANES, CH>([&](int j, float* f) { unpack8(raw[j], f); }, lane, (K + 127) / 128 * 16,
+                             m < M, q + m * ld_q, scale + m, lds, turn);
+}
+
+// 8 consecutive features of an fp32 vector, or `none` where there is none.
+__device__ __forceinline__ void load8(const float* v, int c, bool in, float none, float (&f)[8]) {
+  float4 a = {none, none, none, none}, b = a;
+  if (v && in) {
+    a = reinterpret_cast<const float4*>(v + 8 * c)[0];
+    b = reinterpret_cast<const float4*>(v + 8 * c)[1];
+  }
+  const float t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = t[i];
+}
+
+// The factor and the summand of a lane's features: gamma and beta of a norm,
+// for the norm after the block times the gate.
+template <int LANES, int CH>
+struct Affine {
+  float g[CH][8], b[CH][8];
+  __device__ __forceinline__ void load(const float* gamma, const float* beta, const float* gate, int lane,
+                                       int chunks) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int c = j * LANES + lane;
+      load8(gamma, c, c < chunks, 1.0f, g[j]);
+      load8(beta, c, c < chunks, 0.0f, b[j]);
+      if (gate) {
+        float f[8];
+        load8(gate, c, c < chunks, 0.0f, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          g[j][i] *= f[i];
+          b[j][i] *= f[i];
+        }
+      }
+    }
+  }
+};
+
+// v <- (v - mean) / sqrt(var + eps) over the row, or v / sqrt(mean v^2 + eps).
+// Chunks past the row hold 0 and stay out of the variance.
 template <int LANES, int CH, bool RMS>
-__device__ __forceinline__ void row_norm(float (&v)[CH][8], int lane, int chunks, int d, float eps,
-                                         const float* gamma, const float* beta, float* lds) {
-  const float inv_d = 1.0f / (float)d;
+__device__ __forceinline__ void normalise(float (&v)[CH][8], int lane, int chunks, float inv_d, float eps,
+                                          float (&lds)[2][16], int& turn) {
   float mean = 0.0f, sq = 0.0f;
   if constexpr (!RMS) {
     float s = 0.0f;
@@ -121,125 +197,135 @@ __device__ __forceinline__ void row_norm(float (&v)[CH][8], int lane, int chunks
     for (int j = 0; j < CH; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[j][i];
-    mean = row_reduce<LANES, SUM>(s, lds) * inv_d;
+    mean = row_reduce<LANES, SUM>(s, lds, turn) * inv_d;
   }
 #pragma unroll
   for (int j = 0; j < CH; ++j)
-    if (j * LANES + lane < chunks) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[j][i] -= mean;
-        sq = fmaf(v[j][i], v[j][i], sq);
-      }
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (!RMS) v[j][i] = j * LANES + lane < chunks ? v[j][i] - mean : 0.0f;
+      sq = fmaf(v[j][i], v[j][i], sq);
     }
-  const float rstd = 1.0f / sqrtf(fmaf(row_reduce<LANES, SUM>(sq, lds), inv_d, eps));
+  const float rstd = 1.0f / sqrtf(fmaf(row_reduce<LANES, SUM>(sq, lds, turn), inv_d, eps));
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int c = j * LANES + lane;
-    if (c < chunks) {
-      const float4* g = reinterpret_cast<const float4*>(gamma + 8 * c);
-      const float4 g0 = g[0], g1 = g[1];
-      const float gg[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+  for (int j = 0; j < CH; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] *= rstd * gg[i];
-      if (beta) {
-        const float4* b = reinterpret_cast<const float4*>(beta + 8 * c);
-        const float4 b0 = b[0], b1 = b[1];
-        const float bb[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[j][i] += bb[i];
-      }
-    }
-  }
+    for (int i = 0; i < 8; ++i) v[j][i] *= rstd;
 }
 
+// A lane group works through `turns` rows with the vectors in registers and
+// reads the next row while it works on one; the rows of a workgroup are
+// consecutive (a grid's stride between them: 341 -> 383 us for 200,003 rows of
+// 1024 with gate rows).
 template <int LANES, int CH, bool RMS>
-__global__ __launch_bounds__(BLOCK) void block_norm_kernel(int64_t M, int d, BlockNorm a) {
-  constexpr int ROWS = BLOCK / LANES;
-  __shared__ float lds[4];
+__global__ __launch_bounds__(block_of(LANES)) void block_norm_kernel(int64_t M, int d, int turns, BlockNorm a) {
+  constexpr int ROWS = block_of(LANES) / LANES;               // rows of a workgroup at a time
+  constexpr int PER = LANES < 64 ? 64 / LANES : 1;  // and of a wave
+  __shared__ float lds[2][16];
+  int turn = 0;
   const int lane = threadIdx.x % LANES;
-  const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
-  if (m >= M) return;  // LANES = 256: the whole workgroup
+  const int sub = threadIdx.x / LANES;
   const int chunks = d / 8;
-  const uint4 zero = {0u, 0u, 0u, 0u};
-  uint4 xr[CH], br[CH], gr[CH];
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int c = j * LANES + lane;
-    const bool in = c < chunks;
-    xr[j] = in ? *reinterpret_cast<const uint4*>(a.x + m * a.ld_x + 8 * c) : zero;
-    br[j] = in && a.block ? *reinterpret_cast<const uint4*>(a.block + m * a.ld_block + 8 * c) : zero;
-    gr[j] = in && a.gate_rows ? *reinterpret_cast<const uint4*>(a.gate_rows + m * a.ld_gate + 8 * c)
-                              : zero;
-  }
-  float v[CH][8];
-#pragma unroll
-  for (int j = 0; j < CH; ++j) unpack8(br[j], v[j]);
-  if (a.post_gamma)
-    row_norm<LANES, CH, RMS>(v, lane, chunks, d, a.eps, a.post_gamma, a.post_beta, lds);
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int c = j * LANES + lane;
-    float f[8];
-    if (a.gate_rows) {
-      unpack8(gr[j], f);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] *= f[i];
-    }
-    if (a.gate && c < chunks) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] *= a.gate[8 * c + i];
-    }
-    unpack8(xr[j], f);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] = fmaf(a.res_scale, f[i], v[j][i]);
-    if (a.y && c < chunks) *reinterpret_cast<uint4*>(a.y + m * a.ld_y + 8 * c) = pack8(v[j]);
-  }
-  if (!a.z && !a.zq) return;
-  // The next block's norm reads the stream before its rounding to bf16.
-  row_norm<LANES, CH, RMS>(v, lane, chunks, d, a.eps, a.pre_gamma, a.pre_beta, lds);
-  if (a.z) {
+  const float inv_d = 1.0f / (float)d;
+  const bool norm = a.z || a.zq;
+  struct Row {
+    uint4 x[CH], b[CH], g[CH];
+  };
+  auto read = [&](int64_t m, Row& r) {
+    const uint4 zero = {0u, 0u, 0u, 0u};
+    m = min(m, M - 1);
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
       const int c = j * LANES + lane;
-      if (c < chunks) *reinterpret_cast<uint4*>(a.z + m * a.ld_z + 8 * c) = pack8(v[j]);
+      const bool in = c < chunks;
+      r.x[j] = in ? load16(a.x + m * a.ld_x + 8 * c) : zero;
+      r.b[j] = in && a.block ? load16(a.block + m * a.ld_block + 8 * c) : zero;
+      r.g[j] = in && a.gate_rows ? load16(a.gate_rows + m * a.ld_gate + 8 * c)
+                                 : zero;
     }
-  }
-  if (a.zq) {
-    float amax = 0.0f;
+  };
+  // The rows of this wave (of the workgroup) at each turn start at m0.
+  const int64_t first = (int64_t)blockIdx.x * (ROWS * turns) + sub / PER * PER;
+  const int64_t step = ROWS, end = min(M, ((int64_t)blockIdx.x + 1) * (ROWS * turns));
+  Row cur, next;
+  if (first < M) read(first + sub % PER, cur);
+  Affine<LANES, CH> post, pre;
+  post.load(a.post_gamma, a.post_beta, a.gate, lane, chunks);
+  if (norm) pre.load(a.pre_gamma, a.pre_beta, nullptr, lane, chunks);
+  for (int64_t m0 = first; m0 < end; m0 += step) {
+    const int64_t m = m0 + sub % PER;
+    const bool store = m < M;
+    if (m0 + step < end) read(m + step, next);
+    float v[CH][8], f[8];
+    uint4 y[CH];
 #pragma unroll
-    for (int j = 0; j < CH; ++j) amax = amax8(v[j], amax);
-    amax = row_reduce<LANES, MAX>(amax, lds);
-    const bool bad = amax == INFINITY;
-    const RowScale s = bad ? poisoned() : row_scale(amax);
-    const int padded = (d + 127) / 128 * 16;
+    for (int j = 0; j < CH; ++j) unpack8(cur.b[j], v[j]);
+    if (a.post_gamma) normalise<LANES, CH, RMS>(v, lane, chunks, inv_d, a.eps, lds, turn);
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
       const int c = j * LANES + lane;
-      if (c < padded)
-        *reinterpret_cast<uint2*>(a.zq + m * a.ld_zq + 8 * c) =
-            bad ? uint2{0u, 0u} : quantize8(v[j], s.inv);
+      const bool in = c < chunks;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = in ? fmaf(v[j][i], post.g[j][i], post.b[j][i]) : 0.0f;
+      if (a.gate_rows) {
+        unpack8(cur.g[j], f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] *= f[i];
+      }
+      unpack8(cur.x[j], f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = fmaf(a.res_scale, f[i], v[j][i]);
+      y[j] = pack8(v[j]);
     }
-    if (lane == 0) a.zq_scale[m] = s.scale;
+    if (norm) {
+      // The next block's norm reads the stream before its rounding to bf16.
+      normalise<LANES, CH, RMS>(v, lane, chunks, inv_d, a.eps, lds, turn);
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        const bool in = j * LANES + lane < chunks;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = in ? fmaf(v[j][i], pre.g[j][i], pre.b[j][i]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int c = j * LANES + lane;
+      if (store && c < chunks) {
+        if (a.y) store16(a.y + m * a.ld_y + 8 * c, y[j]);
+        if (a.z) store16(a.z + m * a.ld_z + 8 * c, pack8(v[j]));
+      }
+    }
+    if (a.zq)
+      store_quantized<LANES, CH>(
+          [&](int j, float* t) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = v[j][i];
+          },
+          lane, (d + 127) / 128 * 16, store, a.zq + m * a.ld_zq, a.zq_scale + m, lds, turn);
+    cur = next;
   }
 }
 
 }  // namespace
 
-// The fewest lanes whose 4 chunks (8 beyond 8192 features) hold a padded row:
-// short rows share a wave, rows beyond 2048 features take a workgroup.
+static unsigned groups(int64_t M, int lanes) {
+  const int rows = block_of(lanes) / lanes;
+  return (unsigned)((M + rows - 1) / rows);
+}
+
+// Lanes and chunks that hold a padded row: as few features a lane as fill a
+// wave (rows of up to 256 share one), and a workgroup beyond 1024.
 hipError_t launch_quantize_rows(int64_t M, int K, const uint16_t* x, int64_t ld_x, int8_t* q,
                                 int64_t ld_q, float* scale, hipStream_t stream) {
   if (M <= 0) return hipSuccess;
   const int n = (int)i8_columns(K) / 8;
-#define SURGE_LAUNCH(LANES, CH)                                                               \
-  hipLaunchKernelGGL((quantize_rows_kernel<LANES, CH>),                                       \
-                     dim3((unsigned)((M + BLOCK / LANES - 1) / (BLOCK / LANES))), dim3(BLOCK), \
-                     0, stream, M, K, x, ld_x, q, ld_q, scale)
-  if (n <= 64)
-    SURGE_LAUNCH(16, 4);
-  else if (n <= 128)
-    SURGE_LAUNCH(32, 4);
+#define SURGE_LAUNCH(LANES, CH)                                                         \
+  hipLaunchKernelGGL((quantize_rows_kernel<LANES, CH>), dim3(groups(M, LANES)),          \
+                     dim3(block_of(LANES)), 0, stream, M, K, x, ld_x, q, ld_q, scale)
+  if (n <= 32)
+    SURGE_LAUNCH(16, 2);
+  else if (n <= 64)
+    SURGE_LAUNCH(32, 2);
   else if (n <= 256)
     SURGE_LAUNCH(64, 4);
   else if (n <= 1024)
@@ -250,26 +336,43 @@ hipError_t launch_quantize_rows(int64_t M, int K, const uint16_t* x, int64_t ld_
   return hipGetLastError();
 }
 
-hipError_t launch_block_norm(int64_t M, int d, bool rms, const BlockNorm& a, hipStream_t stream) {
+// Turns: as many as let one round of three workgroups per CU take all rows, so
+// that no few workgroups are left for a second one (13,579 rows of 768: 20.3
+// us, with 4 turns 23.6), and 4 where the rounds are many (200,003 rows of
+// 1024 with gate rows, turns 1 / 2 / 4 / 8: 345 / 341 / 341 / 369; of 768 with
+// a gate 304 / 242 / 227 / 232).  Rows beyond 4096 in 512 lanes of two chunks:
+// 20,000 of 8192 306 us, in 256 of four 323, in 1024 of one 328.
+hipError_t launch_block_norm(int64_t M, int d, bool rms, const BlockNorm& a, int n_cus,
+                             hipStream_t stream) {
   if (M <= 0) return hipSuccess;
   const int n = (int)i8_columns(d) / 8;
-#define SURGE_LAUNCH_KIND(LANES, CH, RMS)                                                     \
-  hipLaunchKernelGGL((block_norm_kernel<LANES, CH, RMS>),                                     \
-                     dim3((unsigned)((M + BLOCK / LANES - 1) / (BLOCK / LANES))), dim3(BLOCK), \
-                     0, stream, M, d, a)
-#define SURGE_LAUNCH(LANES, CH)       \
-  if (rms)                            \
-    SURGE_LAUNCH_KIND(LANES, CH, true); \
-  else                                \
+#define SURGE_LAUNCH_KIND(LANES, CH, RMS)                                                      \
+  {                                                                                            \
+    const int64_t n_groups = groups(M, LANES);                                                 \
+    const int64_t turns = n_groups > 18 * n_cus ? 4 : (n_groups + 3 * n_cus - 1) / (3 * n_cus); \
+    hipLaunchKernelGGL((block_norm_kernel<LANES, CH, RMS>),                                    \
+                       dim3((unsigned)((n_groups + turns - 1) / turns)), dim3(block_of(LANES)), 0, \
+                       stream, M, d, (int)turns, a);                                           \
+  }
+#define SURGE_LAUNCH(LANES, CH)        \
+  if (rms)                             \
+    SURGE_LAUNCH_KIND(LANES, CH, true) \
+  else                                 \
     SURGE_LAUNCH_KIND(LANES, CH, false)
-  if (n <= 64) {
-    SURGE_LAUNCH(16, 4);
+  if (n <= 16) {
+    SURGE_LAUNCH(16, 1);
+  } else if (n <= 32) {
+    SURGE_LAUNCH(32, 1);
+  } else if (n <= 64) {
+    SURGE_LAUNCH(64, 1);
   } else if (n <= 128) {
-    SURGE_LAUNCH(32, 4);
+    SURGE_LAUNCH(64, 2);
   } else if (n <= 256) {
-    SURGE_LAUNCH(64, 4);
+    SURGE_LAUNCH(256, 1);
+  } else if (n <= 512) {
+    SURGE_LAUNCH(256, 2);
   } else {
-    SURGE_LAUNCH(256, 4);
+    SURGE_LAUNCH(512, 2);
   }
 #undef SURGE_LAUNCH
 #undef SURGE_LAUNCH_KIND

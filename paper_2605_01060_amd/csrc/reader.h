@@ -35,7 +35,8 @@ struct BlockNorm {
   int64_t ld_zq;
   float* zq_scale;
 };
-hipError_t launch_block_norm(int64_t M, int d, bool rms, const BlockNorm& a, hipStream_t stream);
+hipError_t launch_block_norm(int64_t M, int d, bool rms, const BlockNorm& a, int n_cus,
+                             hipStream_t stream);
 
 // y[m][n] = epi(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n]), epi 0
 // nothing, 1 GELU, 2 + res[m][n].  K % 128 == 0, N % 8 == 0.

@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 
 #include "cross.h"
@@ -74,6 +75,20 @@ surge_status check_offsets(const char* name, int64_t n, const int64_t* cu) {
   return SURGE_OK;
 }
 
+// The current device and its compute units, asked for once a device.
+surge_status current_device(int* dev, int* n_cus) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int> known[kMaxDevices];
+  HIP_TRY(hipGetDevice(dev));
+  if (*dev < 0 || *dev >= kMaxDevices)
+    return fail(SURGE_ERR_DEVICE, "device index %d outside [0, %d)", *dev, kMaxDevices);
+  *n_cus = known[*dev].load(std::memory_order_relaxed);
+  if (*n_cus > 0) return SURGE_OK;
+  HIP_TRY(resolve_cus(n_cus));
+  known[*dev].store(*n_cus, std::memory_order_relaxed);
+  return SURGE_OK;
+}
+
 #define CHECK(expr)                     \
   do {                                  \
     const surge_status st_ = (expr);    \
@@ -126,8 +141,8 @@ surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d
   CHECK(check_vector("bias", d_bias, true));
   if ((M + 15) / 16 * ((N + 15) / 16) > (int64_t)INT32_MAX)
     return fail(SURGE_ERR_CAPACITY, "M=%lld, N=%d: too many tiles", (long long)M, N);
-  int n_cus = 0;
-  HIP_TRY(resolve_cus(&n_cus));
+  int dev = 0, n_cus = 0;
+  CHECK(current_device(&dev, &n_cus));
   const LinearI8 a = {d_x,    d_w,    ld_x, d_x_scale, d_w_scale, d_bias,
                       d_res, ld_res, d_y,  ld_y};
   HIP_TRY(launch_linear_i8(M, N, K, epilogue, a, n_cus, (hipStream_t)hip_stream));
@@ -184,7 +199,9 @@ surge_status surge_op_block_norm(int64_t M, int32_t d, int32_t kind, const uint1
   const BlockNorm a = {d_x,         d_block,    d_gate_rows, ld_x, ld_block, ld_gate, d_post_gamma,
                        d_post_beta, d_gate,     d_pre_gamma, d_pre_beta, res_scale, eps, d_y, d_z,
                        ld_y,        ld_z,       d_zq,        ld_zq, d_zq_scale};
-  HIP_TRY(launch_block_norm(M, d, kind == SURGE_NORM_RMS, a, (hipStream_t)hip_stream));
+  int dev = 0, n_cus = 0;
+  CHECK(current_device(&dev, &n_cus));
+  HIP_TRY(launch_block_norm(M, d, kind == SURGE_NORM_RMS, a, n_cus, (hipStream_t)hip_stream));
   return SURGE_OK;
 }
 
@@ -208,8 +225,8 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     return fail(SURGE_ERR_CAPACITY, "too many rows of queries and heads");
   try {
     CrossList list;
-    int n_cus = 0;
-    HIP_TRY(resolve_cus(&n_cus));
+    int dev = 0, n_cus = 0;
+    CHECK(current_device(&dev, &n_cus));
     build_cross_list(n_seqs, h_cu_q, h_cu_kv, n_kv_heads, group, d_head, n_cus, &list);
     int64_t items = 0;
     for (const auto& v : list.items) items += (int64_t)v.size();
@@ -227,8 +244,9 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     p->max_parts = list.max_parts;
     p->n_parts = list.n_parts;
     const size_t bytes = items * sizeof(CrossItem) + list.joins.size() * sizeof(CrossJoin);
-    hipError_t e = hipGetDevice(&p->device);
-    if (e == hipSuccess && bytes > 0) e = hipMalloc(&p->lists, bytes);
+    p->device = dev;
+    hipError_t e = hipSuccess;
+    if (bytes > 0) e = hipMalloc(&p->lists, bytes);
     char* at = (char*)p->lists;
     auto upload = [&](const void* from, size_t n) {
       if (e == hipSuccess && n > 0) e = hipMemcpy(at, from, n, hipMemcpyHostToDevice);
