@@ -60,16 +60,15 @@ CrossList split_list(const Lengths& s, int64_t share) {
   return out;
 }
 
-// Units of a class that a CU has at a time (registers and, for 128 rows, LDS),
-// counting those of one wave at the four that keep the memory busy.
-constexpr int PER_CU[CROSS_CLASSES] = {2, 4, 4};
-
 // What a list takes, in us: each class as its units, longest first, go to the
-// first free of the chip's places, then the join.  Measured on full chips, a
-// block of 32 keys takes 128 rows 0.25 + 0.007 d_head us (d_head 32 0.48, 64
-// 0.71, 128 1.13), and a unit about six blocks beside its keys.
+// first free of the chip's places, then the join.  A place is a workgroup that
+// the registers let a CU hold (of one wave the four that keep the memory
+// busy).  Measured on full chips, a block of 32 keys takes 128 rows 0.67, 0.92
+// and 1.10 us (d_head 32, 64, 128), and a unit about six blocks beside its
+// keys.
 double list_us(const CrossList& list, int n_kv_heads, int d_head, int n_cus) {
-  const double block = 0.25 + 0.007 * d_head;
+  const double block = d_head == 32 ? 0.67 : d_head == 64 ? 0.92 : 1.10;
+  const int per_cu[CROSS_CLASSES] = {d_head == 128 ? 2 : 3, 4, 4};
   double us = 0;
   for (int c = 0; c < CROSS_CLASSES; ++c) {
     std::priority_queue<double, std::vector<double>, std::greater<double>> places;
@@ -77,7 +76,7 @@ double list_us(const CrossList& list, int n_kv_heads, int d_head, int n_cus) {
     for (const CrossItem& it : list.items[c])
       for (int h = 0; h < n_kv_heads; ++h) {
         double t = (double)(blocks32(it.k1 - it.k0) + 6) * block;
-        if ((int)places.size() == PER_CU[c] * n_cus) {
+        if ((int)places.size() == per_cu[c] * n_cus) {
           t += places.top();
           places.pop();
         }

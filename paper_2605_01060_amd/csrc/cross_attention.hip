@@ -28,28 +28,35 @@
 namespace surge {
 namespace {
 
-// Chunk c of LDS row r (DH bf16) is stored at c ^ f(r): as swz() for rows of
-// 4 or 8 chunks, r & 15 for 16, so that the 16 lanes that the LDS serves
-// together in a read of one chunk from 32 rows fall on slots of their own.
+// LDS rows of CPR 16-byte chunks (DH bf16); chunk c of row r is stored at
+// position c ^ f(r), with
+//   CPR = 16: f(r) = 4 (r & 3) + (r / 4 & 3),
+//   CPR = 8:  f(r) = 4 (r / 2 & 1) + (r / 4 & 3),
+//   CPR = 4:  as swz().
+// Two reads are served without bank conflicts: K's, one chunk of 32 rows (the
+// 16 lanes that the LDS serves together fall on slots of their own, as f takes
+// each value for rows of one position), and V's transposing read, whose 32
+// lanes take 64 bytes of each of four consecutive rows: bit 2 and up of f put
+// them on different 64 bytes.  (With f(r) = r & 15 and swz<8>() the latter
+// were conflicts, 59 and 32 % of the LDS's busy cycles.)
 template <int CPR>
 __device__ __forceinline__ int kv_slot(int row, int chunk) {
-  if constexpr (CPR == 16)
-    return row * 16 + (chunk ^ (row & 15));
-  else
-    return swz<CPR>(row, chunk);
+  if constexpr (CPR == 16) return row * 16 + (chunk ^ ((row & 3) << 2 | (row >> 2 & 3)));
+  if constexpr (CPR == 8) return row * 8 + (chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3)));
+  return swz<4>(row, chunk);
 }
+// The logical chunk of the slot that lane l fills with copy `copy` of a block.
 template <int CPR>
 __device__ __forceinline__ int kv_copy_chunk(int lane, int copy) {
-  if constexpr (CPR == 16)
-    return (lane & 15) ^ ((4 * copy + (lane >> 4)) & 15);
-  else
-    return copy_chunk<CPR>(lane, copy);
+  if constexpr (CPR == 16) return (lane & 15) ^ ((lane >> 4) << 2 | (copy & 3));
+  if constexpr (CPR == 8) return (lane & 7) ^ ((lane >> 4 & 1) << 2 | (copy & 1) << 1 | lane >> 5);
+  return copy_chunk<4>(lane, copy);
 }
 
 // WAVES waves of 32 rows against blocks of KB keys that they share in LDS, the
 // next block copied while the current one is on the MFMA units.
 template <int DH, int WAVES, int KB>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void cross_kernel(
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 2 : 3))) void cross_kernel(
     CrossAttention a, const CrossItem* items) {
   constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8;
   constexpr int RPC = 64 / CPR;          // rows that a copy instruction fills
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
   const int tr_feat = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   uint32_t ka = lds + (uint32_t)kv_slot<CPR>(col, half) * 16u;
   uint32_t va = lds + 2 * BUF + (uint32_t)kv_slot<CPR>(tr_key, tr_feat >> 3) * 16u + (tr_feat & 7) * 2u;
-  constexpr uint32_t H_SWZ = CPR == 16 ? 128 : 16;  // of 8 keys further on
+  constexpr uint32_t H_SWZ = CPR == 4 ? 16 : 32;  // of 8 keys further on
   auto k_fragment = [&](int t, int kk) {
     return __builtin_bit_cast(
         bf16x8, *(const __attribute__((address_space(3))) u32x4*)((ka ^ kk * 32) + t * 32 * ROW));
@@ -157,6 +164,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
     }
     if (active && keys) {
       f32x16 s[T];
+      // Ahead of the waves of the SIMD that are at their exponentials.
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -166,6 +175,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
         for (int t = 0; t < T; ++t)
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
+      __builtin_amdgcn_s_setprio(0);
       if (keys != FULL) {
 #pragma unroll
         for (int t = 0; t < T; ++t)
