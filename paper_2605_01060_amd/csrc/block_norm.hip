@@ -135,17 +135,19 @@ __global__ __launch_bounds__(block_of(LANES)) void quantize_rows_kernel(int64_t 
   __shared__ float lds[2][16];
   int turn = 0;
   const int lane = threadIdx.x % LANES;
-  const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
   const int chunks = K / 8;
-  const uint16_t* xr = x + min(m, M - 1) * ld_x;
-  uint4 raw[CH];
+  for (int64_t m0 = (int64_t)blockIdx.x * ROWS; m0 < M; m0 += (int64_t)gridDim.x * ROWS) {
+    const int64_t m = m0 + threadIdx.x / LANES;
+    const uint16_t* xr = x + min(m, M - 1) * ld_x;
+    uint4 raw[CH];
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int c = j * LANES + lane;
-    raw[j] = c < chunks ? load16(xr + 8 * c) : uint4{0u, 0u, 0u, 0u};
+    for (int j = 0; j < CH; ++j) {
+      const int c = j * LANES + lane;
+      raw[j] = c < chunks ? load16(xr + 8 * c) : uint4{0u, 0u, 0u, 0u};
+    }
+    store_quantized<LANES, CH>([&](int j, float* f) { unpack8(raw[j], f); }, lane, (K + 127) / 128 * 16,
+                               m < M, q + m * ld_q, scale + m, lds, turn);
   }
-  store_quantized<LANES, CH>([&](int j, float* f) { unpack8(raw[j], f); }, lane, (K + 127) / 128 * 16,
-                             m < M, q + m * ld_q, scale + m, lds, turn);
 }
 
 // 8 consecutive features of an fp32 vector, or `none` where there is none.
@@ -308,10 +310,13 @@ __global__ __launch_bounds__(block_of(LANES)) void block_norm_kernel(int64_t M, 
 
 }  // namespace
 
-static unsigned groups(int64_t M, int lanes) {
+static int64_t groups(int64_t M, int lanes) {
   const int rows = block_of(lanes) / lanes;
-  return (unsigned)((M + rows - 1) / rows);
+  return (M + rows - 1) / rows;
 }
+
+// Most workgroups of a launch: a grid's threads are a 32-bit number.
+constexpr int64_t MOST_GROUPS = 1 << 22;
 
 // Lanes and chunks that hold a padded row: as few features a lane as fill a
 // wave (rows of up to 256 share one), and a workgroup beyond 1024.
@@ -320,7 +325,7 @@ hipError_t launch_quantize_rows(int64_t M, int K, const uint16_t* x, int64_t ld_
   if (M <= 0) return hipSuccess;
   const int n = (int)i8_columns(K) / 8;
 #define SURGE_LAUNCH(LANES, CH)                                                         \
-  hipLaunchKernelGGL((quantize_rows_kernel<LANES, CH>), dim3(groups(M, LANES)),          \
+  hipLaunchKernelGGL((quantize_rows_kernel<LANES, CH>), dim3((unsigned)std::min(groups(M, LANES), MOST_GROUPS)), \
                      dim3(block_of(LANES)), 0, stream, M, K, x, ld_x, q, ld_q, scale)
   if (n <= 32)
     SURGE_LAUNCH(16, 2);
@@ -349,7 +354,9 @@ hipError_t launch_block_norm(int64_t M, int d, bool rms, const BlockNorm& a, int
 #define SURGE_LAUNCH_KIND(LANES, CH, RMS)                                                      \
   {                                                                                            \
     const int64_t n_groups = groups(M, LANES);                                                 \
-    const int64_t turns = n_groups > 18 * n_cus ? 4 : (n_groups + 3 * n_cus - 1) / (3 * n_cus); \
+    const int64_t turns = n_groups > 18 * n_cus                                                \
+                              ? std::max<int64_t>(4, (n_groups + MOST_GROUPS - 1) / MOST_GROUPS) \
+                              : (n_groups + 3 * n_cus - 1) / (3 * n_cus);                      \
     hipLaunchKernelGGL((block_norm_kernel<LANES, CH, RMS>),                                    \
                        dim3((unsigned)((n_groups + turns - 1) / turns)), dim3(block_of(LANES)), 0, \
                        stream, M, d, (int)turns, a);                                           \

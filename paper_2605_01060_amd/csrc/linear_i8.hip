@@ -617,18 +617,28 @@ hipError_t launch(int64_t M, int N, int K, const LinearI8& a, int n_cus, hipStre
 }  // namespace
 
 int linear_i8_tile(int64_t M, int N, int K, int n_cus) {
-  const Cost& q = COSTS[choose(M, N, K, n_cus)];
+  const Cost& q = COSTS[choose(std::min<int64_t>(M, 1 << 24), N, K, n_cus)];
   return q.rows << 16 | q.cols;
 }
 
+// Rows in launches of at most 2^24, so that row numbers and grids stay well
+// inside 32 bits.
 hipError_t launch_linear_i8(int64_t M, int N, int K, int epi, const LinearI8& a, int n_cus,
                             hipStream_t stream) {
-  if (M <= 0) return hipSuccess;
-  switch (epi) {
-    case EPI_BIAS: return launch<EPI_BIAS>(M, N, K, a, n_cus, stream);
-    case EPI_BIAS_GELU: return launch<EPI_BIAS_GELU>(M, N, K, a, n_cus, stream);
-    default: return launch<EPI_BIAS_RESIDUAL>(M, N, K, a, n_cus, stream);
+  constexpr int64_t MOST = 1 << 24;
+  for (int64_t m = 0; m < M; m += MOST) {
+    const int64_t rows = std::min(MOST, M - m);
+    LinearI8 part = a;
+    part.x += m * a.ld_x;
+    part.x_scale += m;
+    if (part.res) part.res += m * a.ld_res;
+    part.y += m * a.ld_y;
+    const hipError_t e = epi == EPI_BIAS        ? launch<EPI_BIAS>(rows, N, K, part, n_cus, stream)
+                         : epi == EPI_BIAS_GELU ? launch<EPI_BIAS_GELU>(rows, N, K, part, n_cus, stream)
+                                                : launch<EPI_BIAS_RESIDUAL>(rows, N, K, part, n_cus, stream);
+    if (e != hipSuccess) return e;
   }
+  return hipSuccess;
 }
 
 }  // namespace surge

@@ -63,23 +63,33 @@ surge_status check_rows(int64_t M) {
   return SURGE_OK;
 }
 
-// cu[0] = 0, never decreasing, at most INT32_MAX rows.
+// Rows of queries and of keys are counted in 32 bits, a block of them beyond
+// the last one too.
+constexpr int64_t kMostRows = INT32_MAX - 255;
+
+// cu[0] = 0, never decreasing, at most kMostRows.
 surge_status check_offsets(const char* name, int64_t n, const int64_t* cu) {
   if (!cu) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s is NULL", name);
   if (cu[0] != 0) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s[0] != 0", name);
   for (int64_t i = 0; i < n; ++i)
     if (cu[i + 1] < cu[i])
       return fail(SURGE_ERR_INVALID_ARGUMENT, "%s decreases at %lld", name, (long long)i);
-  if (cu[n] > (int64_t)INT32_MAX)
-    return fail(SURGE_ERR_INVALID_ARGUMENT, "%s: too many rows", name);
+  if (cu[n] > kMostRows) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s: too many rows", name);
   return SURGE_OK;
 }
 
-// The current device and its compute units, asked for once a device.
-surge_status current_device(int* dev, int* n_cus) {
+// The current device and its compute units, asked for once a device, and that
+// the stream is one of this device's.
+surge_status current_device(hipStream_t stream, int* dev, int* n_cus) {
   constexpr int kMaxDevices = 64;
   static std::atomic<int> known[kMaxDevices];
   HIP_TRY(hipGetDevice(dev));
+  if (stream) {
+    int own = 0;
+    HIP_TRY(hipStreamGetDevice(stream, &own));
+    if (own != *dev)
+      return fail(SURGE_ERR_INVALID_ARGUMENT, "a stream of device %d, the current one is %d", own, *dev);
+  }
   if (*dev < 0 || *dev >= kMaxDevices)
     return fail(SURGE_ERR_DEVICE, "device index %d outside [0, %d)", *dev, kMaxDevices);
   *n_cus = known[*dev].load(std::memory_order_relaxed);
@@ -115,6 +125,8 @@ surge_status surge_op_quantize_rows(int64_t M, int32_t K, const uint16_t* d_x, i
   CHECK(check_matrix("x", d_x, K, ld_x, 8));
   CHECK(check_matrix("q", d_q, i8_columns(K), ld_q, 16));
   if (!d_scale) return fail(SURGE_ERR_INVALID_ARGUMENT, "scale is NULL");
+  int dev = 0, n_cus = 0;
+  CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   HIP_TRY(launch_quantize_rows(M, K, d_x, ld_x, d_q, ld_q, d_scale, (hipStream_t)hip_stream));
   return SURGE_OK;
 }
@@ -139,10 +151,8 @@ surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d
   CHECK(check_vector("w", d_w, true));
   CHECK(check_vector("w_scale", d_w_scale, true));
   CHECK(check_vector("bias", d_bias, true));
-  if ((M + 15) / 16 * ((N + 15) / 16) > (int64_t)INT32_MAX)
-    return fail(SURGE_ERR_CAPACITY, "M=%lld, N=%d: too many tiles", (long long)M, N);
   int dev = 0, n_cus = 0;
-  CHECK(current_device(&dev, &n_cus));
+  CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   const LinearI8 a = {d_x,    d_w,    ld_x, d_x_scale, d_w_scale, d_bias,
                       d_res, ld_res, d_y,  ld_y};
   HIP_TRY(launch_linear_i8(M, N, K, epilogue, a, n_cus, (hipStream_t)hip_stream));
@@ -200,7 +210,7 @@ surge_status surge_op_block_norm(int64_t M, int32_t d, int32_t kind, const uint1
                        d_post_beta, d_gate,     d_pre_gamma, d_pre_beta, res_scale, eps, d_y, d_z,
                        ld_y,        ld_z,       d_zq,        ld_zq, d_zq_scale};
   int dev = 0, n_cus = 0;
-  CHECK(current_device(&dev, &n_cus));
+  CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   HIP_TRY(launch_block_norm(M, d, kind == SURGE_NORM_RMS, a, n_cus, (hipStream_t)hip_stream));
   return SURGE_OK;
 }
@@ -220,18 +230,23 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
   CHECK(check_offsets("cu_q", n_seqs, h_cu_q));
   CHECK(check_offsets("cu_kv", n_seqs, h_cu_kv));
   const int group = n_heads / n_kv_heads;
-  // Rows, and 32 rows and every key head of each unit, are 32-bit numbers.
-  if (h_cu_q[n_seqs] * group > (int64_t)INT32_MAX)
+  if (h_cu_q[n_seqs] * group > kMostRows)
     return fail(SURGE_ERR_CAPACITY, "too many rows of queries and heads");
   try {
     CrossList list;
     int dev = 0, n_cus = 0;
-    CHECK(current_device(&dev, &n_cus));
+    CHECK(current_device(nullptr, &dev, &n_cus));
     build_cross_list(n_seqs, h_cu_q, h_cu_kv, n_kv_heads, group, d_head, n_cus, &list);
+    // A launch's threads are a 32-bit number, two waves for each 32 rows of a
+    // unit at most and sixteen for a joined row.
     int64_t items = 0;
-    for (const auto& v : list.items) items += (int64_t)v.size();
-    if (std::max(items, 32 * (int64_t)list.joins.size()) * n_kv_heads > (int64_t)INT32_MAX)
-      return fail(SURGE_ERR_CAPACITY, "too many units of 32 rows");
+    bool fits = (int64_t)list.joins.size() * n_kv_heads <= (1 << 16);
+    for (int c = 0; c < CROSS_CLASSES; ++c) {
+      items += (int64_t)list.items[c].size();
+      fits = fits && (int64_t)list.items[c].size() * n_kv_heads * CROSS_ROWS[c] <= (int64_t)INT32_MAX;
+    }
+    if (!fits || items > (int64_t)INT32_MAX)
+      return fail(SURGE_ERR_CAPACITY, "too many units of work for one plan");
     surge_cross_plan* p = new surge_cross_plan;
     p->n_kv_heads = n_kv_heads;
     p->group = group;
@@ -315,8 +330,8 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
       return fail(SURGE_ERR_CAPACITY, "workspace of %lld bytes, %lld are needed",
                   (long long)n_workspace, (long long)need);
   }
-  int dev = 0;
-  HIP_TRY(hipGetDevice(&dev));
+  int dev = 0, n_cus = 0;
+  CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   if (dev != plan->device)
     return fail(SURGE_ERR_INVALID_ARGUMENT, "the plan was made on device %d, the current one is %d",
                 plan->device, dev);

@@ -236,6 +236,41 @@ def test_linear_i8_of_a_row_that_could_not_be_quantized():
     assert torch.isfinite(y).all()
 
 
+def test_linear_i8_of_more_rows_than_a_launch_takes():
+    torch = torch_cuda()
+    M, N, K = (1 << 24) + 37, 8, 128
+    p = linear_inputs(M, N, K, 21)
+    y = p["res"].clone()
+    S.surge_op_linear_i8(M, N, K, p["x"], K, p["xs"], p["w"], p["ws"], p["bias"], y, N, 2, y, N,
+                         torch.cuda.current_stream())
+    rows = torch.cat([torch.arange(0, M, 50_021), torch.arange((1 << 24) - 300, M)]).cuda()
+    ref, tol = linear_reference(p, 2, rows)
+    within(y[rows], ref, tol)
+
+
+def test_quantize_rows_and_norms_of_more_rows_than_a_grid_takes():
+    """Rows of 8 features: 2^22 workgroups of 16 rows, the norm's four times over."""
+    torch = torch_cuda()
+    M = (1 << 26) + 21
+    g = gen(22)
+    x = torch.empty(M, 8, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    rows = torch.cat([torch.arange(0, M, 1_000_003), torch.arange((1 << 26) - 40, M)]).cuda()
+    q = torch.empty(M, 128, dtype=torch.int8, device="cuda")
+    scale = torch.empty(M, device="cuda")
+    S.surge_op_quantize_rows(M, 8, x, 8, q, 128, scale, torch.cuda.current_stream())
+    rq, rs = quantized32(x[rows])
+    assert torch.equal(q[rows][:, :8].cpu(), rq) and torch.equal(scale[rows].cpu(), rs)
+    del q, scale
+    M = (1 << 28) + 21
+    rows = torch.cat([torch.arange(0, M, 4_000_037), torch.arange((1 << 28) - 40, M)]).cuda()
+    x = torch.empty(M, 8, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    p = norm_inputs(1, 8, True, False, "none", False, 22)
+    z = torch.empty(M, 8, dtype=torch.bfloat16, device="cuda")
+    block_norm({**p, "x": x}, M, 8, S.NORM_LAYER, 1.0, None, z)
+    _, _, rz, ez = norm_reference({**p, "x": x[rows]}, True, 1.0, 8)
+    within(z[rows], rz, BF16 * rz.abs() + 1.01 * ez)
+
+
 # ---------------------------------------------------------------------------
 # Block norm
 # ---------------------------------------------------------------------------

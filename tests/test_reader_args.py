@@ -41,7 +41,6 @@ LINEAR = dict(M=3, N=24, K=128, d_x=A, ld_x=128, d_x_scale=A, d_w=A, d_w_scale=A
     dict(d_bias=0), dict(d_res=0), dict(d_y=0), dict(d_x=A + 4), dict(d_w=A + 8),
     dict(d_w_scale=A + 4), dict(d_bias=A + 8), dict(d_res=A + 2), dict(d_y=A + 8), dict(ld_x=112),
     dict(ld_x=136), dict(ld_y=16), dict(ld_y=28), dict(ld_res=16), dict(ld_x=1 << 23),
-    dict(M=(1 << 31) - 1, N=1 << 20, ld_y=1 << 20, epilogue=0),
 ])
 def test_linear_i8_refuses(change):
     refused(S.surge_op_linear_i8, LINEAR, **change)
