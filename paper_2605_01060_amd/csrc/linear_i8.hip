@@ -498,6 +498,101 @@ __global__ __launch_bounds__(512) void linear_i8_tokens_kernel(LinearI8 a, int M
                      *reinterpret_cast<const float4*>(a.bias + n), res);
 }
 
+// Few tiles and a long K: 64 tokens x 64 channels a workgroup, every fourth
+// 128-byte stage of K in each of its four waves, which have two stages of LDS
+// of their own and meet only to add up.
+template <int EPI>
+__global__ __launch_bounds__(256) void linear_i8_split_kernel(LinearI8 a, int M, int N, int K, int tiles_n,
+                                                              int n_tiles) {
+  constexpr int WAVES = 4, F = 4;   // fragments of 16 either way
+  constexpr int SLOTS = 128 * 8;    // of a wave's stage
+  __shared__ __attribute__((aligned(128))) u32x4 smem[WAVES * 2 * SLOTS];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, lq = lane >> 4;
+  int tm, tn;
+  tile_coords<ORDER_ROW_GROUPS>(blockIdx.x, n_tiles, tiles_n, &tm, &tn);
+  const int m0 = tm * 64, n0 = tn * 64;
+  const int8_t* xs = a.x + (int64_t)m0 * a.ld_x;
+  const int8_t* ws = a.w + (int64_t)n0 * K;
+  // Copy j fills rows 8 j .. + 7 of either operand; rows past the matrix are
+  // read clamped and never stored.
+  uint32_t xo[8], wo[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int row = j * 8 + (lane >> 3);
+    xo[j] = (uint32_t)min(row, M - 1 - m0) * (uint32_t)a.ld_x + copy_chunk16(lane) * 16u;
+    wo[j] = (uint32_t)min(row, N - 1 - n0) * (uint32_t)K + copy_chunk16(lane) * 16u;
+  }
+  const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem) + wave * (2 * SLOTS * 16));
+  const int nkt = K / 128;
+  auto issue = [&](int kt, int b) {
+    const uint32_t base = lds + b * (SLOTS * 16);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) copy_to_lds16_at(xs + kt * 128, xo[j], base + j * 1024);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) copy_to_lds16_at(ws + kt * 128, wo[j], base + 8192 + j * 1024);
+  };
+  i32x4 acc[F][F];
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  int b = 0;
+  if (wave < nkt) issue(wave, 0);
+  for (int kt = wave; kt < nkt; kt += WAVES, b ^= 1) {
+    if (kt + WAVES < nkt) {
+      issue(kt + WAVES, b ^ 1);  // its last reads were waited for below
+      asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    const u32x4* sx = smem + (wave * 2 + b) * SLOTS;
+    const u32x4* sw = sx + 64 * 8;
+    i32x4 fw[2][F], fx[2][F];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        fw[ks][i] = __builtin_bit_cast(i32x4, sw[swz16(i * 16 + l16, ks * 4 + lq)]);
+        fx[ks][i] = __builtin_bit_cast(i32x4, sx[swz16(i * 16 + l16, ks * 4 + lq)]);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j) acc[i][j] = mma(fw[ks][i], fx[ks][j], acc[i][j]);
+  }
+  __syncthreads();  // every wave has read its stages
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+      smem[((wave * F + j) * F + i) * 64 + lane] = __builtin_bit_cast(u32x4, acc[i][j]);
+  __syncthreads();
+  // Wave j finishes token fragment j.
+  const int m = m0 + wave * 16 + l16;
+  if (m >= M) return;
+  const float sx = a.x_scale[m];
+#pragma unroll
+  for (int i = 0; i < F; ++i) {
+    const int n = n0 + i * 16 + 4 * lq;
+    if (n >= N) continue;
+    i32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w)
+      v += __builtin_bit_cast(i32x4, smem[((w * F + wave) * F + i) * 64 + lane]);
+    uint2 res = {0u, 0u};
+    if constexpr (EPI == EPI_BIAS_RESIDUAL)
+      res = *reinterpret_cast<const uint2*>(a.res + (int64_t)m * a.ld_res + n);
+    *reinterpret_cast<uint2*>(a.y + (int64_t)m * a.ld_y + n) =
+        finish_i8<EPI>(v, sx, *reinterpret_cast<const float4*>(a.w_scale + n),
+                       *reinterpret_cast<const float4*>(a.bias + n), res);
+  }
+}
+
 template <int WAVES_M, int WAVES_N, int TJ, int STAGES, int EPI>
 void launch_ring(int64_t M, int N, int K, const LinearI8& a, hipStream_t stream) {
   constexpr int BM = WAVES_M * TJ * 16, BN = WAVES_N * 64;
@@ -530,9 +625,9 @@ void launch_wide(int64_t M, int N, int K, const LinearI8& a, int n_cus, hipStrea
 //   base + r (round + round_s s) + c (tile + tile_s s) us:
 // what a round's latencies cost, and what tiles that share a CU cost each
 // other.  Fitted to 1,275 launches of 250 shapes (M = 1 .. 60,000, N = 128 ..
-// 4096, K = 128 .. 4096, each under every kernel): 5 to 9 % of the time in the
-// mean square, and the kernel taken is 0.9 % slower than the shape's best in
-// the mean, 25 % at worst.  Measured (us, tokens / 64 x 64 / 64 x 128 / 128 x
+// 4096, K = 128 .. 4096, each under every kernel but the split one): 5 to 9 %
+// of the time in the mean square, and the kernel taken is 0.9 % slower than
+// the shape's best in the mean, 25 % at worst.  Measured (us, tokens / 64 x 64 / 64 x 128 / 128 x
 // 128 / 192 x 256 / 256 x 256):
 //   N = 768, K = 768    M = 1 2.7 / 4.2 / 4.6 / 6.3 / 10.4 / 12.5
 //                       1024 11.1 / 4.7 / 5.1 / 6.8 / 11.1 / 13.2
@@ -540,16 +635,20 @@ void launch_wide(int64_t M, int N, int K, const LinearI8& a, int n_cus, hipStrea
 //   N = 2304, K = 768   M = 1500 39.4 / 8.8 / 7.0 / 8.0 / 11.7 / 14.0
 //                       6000 145 / 23.7 / 21.9 / 18.2 / 22.0 / 16.2
 //   N = 1024, K = 4096  M = 1 4.2 / 11.2 / 13.1 / 18.9 / 32.6 / 40.2
-//                       20,000 1,091 / 119 / 101 / 88.1 / 78.5 / 90.0.
-enum Kernel { TOKENS, RING_64x64, RING_64x128, RING_128x128, WIDE_192, WIDE_256, KERNELS };
+//                       20,000 1,091 / 119 / 101 / 88.1 / 78.5 / 90.0,
+// and with K split over a tile's waves against the 64 x 64 ring: N = 1024, K =
+// 4096 M = 200 8.6 / 11.5, 1024 10.1 / 12.4, 1500 (two tiles on a CU) 17.3 /
+// 14.7; K = 768 M = 777 5.1 / 4.6.
+enum Kernel { TOKENS, SPLIT_64x64, RING_64x64, RING_64x128, RING_128x128, WIDE_192, WIDE_256, KERNELS };
 struct Cost {
   int rows, cols, per_cu;
   double base, round, round_s, tile, tile_s;
 };
 constexpr Cost COSTS[KERNELS] = {
-    {16, 16, 3, 2.1, 0.09, 0.0, 0.08, 0.10},    {64, 64, 3, 2.1, 0.62, 0.14, 0.35, 0.12},
-    {64, 128, 2, 1.6, 1.02, 0.08, 0.48, 0.25},  {128, 128, 2, 0.6, 2.39, 0.17, 0.83, 0.36},
-    {192, 256, 1, 0.2, 0.0, 0.0, 5.50, 0.91},   {256, 256, 1, 0.0, 0.0, 0.0, 6.70, 1.13},
+    {16, 16, 3, 2.1, 0.09, 0.0, 0.08, 0.10},   {64, 64, 1, 0.4, 0.0, 0.0, 3.60, 0.18},
+    {64, 64, 3, 2.1, 0.62, 0.14, 0.35, 0.12},  {64, 128, 2, 1.6, 1.02, 0.08, 0.48, 0.25},
+    {128, 128, 2, 0.6, 2.39, 0.17, 0.83, 0.36}, {192, 256, 1, 0.2, 0.0, 0.0, 5.50, 0.91},
+    {256, 256, 1, 0.0, 0.0, 0.0, 6.70, 1.13},
 };
 
 double kernel_us(Kernel k, int64_t M, int N, int K, int n_cus) {
@@ -596,6 +695,12 @@ hipError_t launch(int64_t M, int N, int K, const LinearI8& a, int n_cus, hipStre
       hipLaunchKernelGGL((linear_i8_tokens_kernel<EPI>), dim3((N + 15) / 16, (unsigned)((M + 15) / 16)),
                          dim3(512), 0, stream, a, (int)M, N, K);
       return hipGetLastError();
+    case SPLIT_64x64: {
+      const int tiles_n = (N + 63) / 64, n_tiles = (int)((M + 63) / 64 * tiles_n);
+      hipLaunchKernelGGL((linear_i8_split_kernel<EPI>), dim3(n_tiles), dim3(256), 0, stream, a, (int)M, N, K,
+                         tiles_n, n_tiles);
+      return hipGetLastError();
+    }
     case RING_64x64: launch_ring<2, 1, 2, 3, EPI>(M, N, K, a, stream); return hipGetLastError();
     case RING_64x128: launch_ring<2, 2, 2, 3, EPI>(M, N, K, a, stream); return hipGetLastError();
     case RING_128x128: launch_ring<2, 2, 4, 2, EPI>(M, N, K, a, stream); return hipGetLastError();

@@ -150,7 +150,8 @@ def test_linear_i8(M, N, K, epi):
 
 # (rows, channels) of the tile, and shapes that take it on 256 compute units;
 # the last two leave channels over for a second launch.
-TILES = [((16, 16), 33, 1000, 768), ((64, 64), 300, 1000, 384), ((64, 128), 777, 1536, 384),
+TILES = [((16, 16), 33, 1000, 768), ((64, 64), 300, 1000, 384), ((64, 64), 700, 520, 4096),
+         ((64, 128), 777, 1536, 384),
          ((128, 128), 4100, 1032, 256), ((192, 256), 13_579, 768, 768), ((256, 256), 6000, 2304, 768),
          ((192, 256), 20_000, 1032, 1024), ((256, 256), 30_000, 1288, 2048)]
 
