@@ -60,70 +60,96 @@ CrossList split_list(const Lengths& s, int64_t share) {
   return out;
 }
 
+// What a unit of a class takes, measured (us): `chain` for a block of 32 keys
+// where it is alone, `full` where the chip is full of such units, `places` of
+// them on a CU (registers and LDS), and `base` beside its keys.  The units of
+// one or two waves are bound by the stream of their keys where they are many.
+struct UnitCost {
+  int places;
+  double base, chain, full;
+};
+const UnitCost& unit_cost(int cls, int d_head) {
+  static const UnitCost costs[CROSS_CLASSES][3] = {
+      {{5, 2.9, 0.31, 0.98}, {4, 3.2, 0.47, 1.13}, {2, 4.3, 0.60, 1.03}},
+      {{14, 2.6, 0.47, 0.47}, {8, 3.0, 0.58, 0.58}, {4, 3.7, 0.80, 0.80}},
+      {{19, 2.4, 0.46, 0.46}, {9, 2.5, 0.62, 0.62}, {4, 2.9, 0.94, 0.94}},
+  };
+  return costs[cls][d_head / 64];
+}
+
 // What a list takes, in us: each class as its units, longest first, go to the
-// first free of the chip's places, then the join.  A place is a workgroup that
-// the registers let a CU hold (of one wave the four that keep the memory
-// busy).  Measured on full chips, a block of 32 keys takes 128 rows 0.67, 0.92
-// and 1.10 us (d_head 32, 64, 128), and a unit about six blocks beside its
-// keys.
+// first free of the chip's places, or as its keys come from memory, then the
+// join.
 double list_us(const CrossList& list, int n_kv_heads, int d_head, int n_cus) {
-  const double block = d_head == 32 ? 0.67 : d_head == 64 ? 0.92 : 1.10;
-  const int per_cu[CROSS_CLASSES] = {d_head == 128 ? 2 : 3, 4, 4};
   double us = 0;
   for (int c = 0; c < CROSS_CLASSES; ++c) {
+    const int64_t units = (int64_t)list.items[c].size() * n_kv_heads;
+    if (units == 0) continue;
+    const UnitCost& q = unit_cost(c, d_head);
+    const double load = std::min(1.0, (double)units / ((double)n_cus * q.places));
+    const double block = std::max(q.chain, q.full * load);
     std::priority_queue<double, std::vector<double>, std::greater<double>> places;
-    double end = 0;
-    for (const CrossItem& it : list.items[c])
+    double end = 0, keys = 0;
+    for (const CrossItem& it : list.items[c]) {
+      keys += it.k1 - it.k0;
       for (int h = 0; h < n_kv_heads; ++h) {
-        double t = (double)(blocks32(it.k1 - it.k0) + 6) * block;
-        if ((int)places.size() == per_cu[c] * n_cus) {
+        double t = q.base + (double)blocks32(it.k1 - it.k0) * block;
+        if ((int)places.size() == q.places * n_cus) {
           t += places.top();
           places.pop();
         }
         places.push(t);
         end = std::max(end, t);
       }
+    }
+    if (c > 0) end = std::max(end, q.base + keys * n_kv_heads * d_head * 4 / 4.9e6);
     us += end;
   }
-  if (list.n_parts > 0) us += 5 + (double)list.n_parts * n_kv_heads * 32 * (d_head * 8 + 16) / 4e6;
+  if (list.n_parts > 0)
+    us += 2.7 + (double)list.n_parts * n_kv_heads * 32 * (d_head * 8 + 16) / 4e6;
   return us;
 }
 
 }  // namespace
 
-// No unit has more than its share of the key blocks, a share being what one
-// of 4 to 8 waves per CU would have of all of them, and at least 8 (256
-// keys).  Few large units leave CUs idle at the end, many cost the join, and
-// which is less depends on the lengths: where the units are few the list with
-// the least time by list_us is taken.  Measured (us, 4 / 6 / 8 waves per CU): heads
-// 16 / 4 x 128, four texts of about 6000, 1500 queries each, 313 / 343 / 345;
-// 16 x 64, 7 texts of about 5000, 300 queries, 160 / 162 / 136; 12 x 64, two
-// of about 9000, 2000 queries, 121 / 91 / 111; 12 x 32, one of 4000, 500
-// queries, 20.8 / 17.8 / 23.1.  One wave's units are bound by the stream of
-// the keys, which 4 per CU keep up best: 16 x 64, three texts of about 20,000,
-// one query, 47.7 / 52.8 / 53.0.
+// A unit has at most its share of the key blocks, a share being what one of 4
+// to 8 waves per CU would have of all of them, and at least two, or all keys
+// of its rows.  Few large units leave CUs idle at the end or wait for one
+// wave's chain of blocks, many cost the join, and which is less depends on the
+// lengths: the list with the least time by list_us is taken.  Measured (us, 4
+// / 6 / 8 waves per CU): heads 16 / 4 x 128, four texts of about 6000, 1500
+// queries each, 313 / 343 / 345; 16 x 64, 7 texts of about 5000, 300 queries,
+// 160 / 162 / 136; 12 x 64, two of about 9000, 2000 queries, 121 / 91 / 111.
+// One query over 512 keys, 12 x 64, shares of 2 / 4 / 8 blocks: 6.4 / 7.2 /
+// 9.6.  64 texts of about 96 keys, one query, 16 x 64: whole 9.6, shares of 4
+// blocks 12.0.
 void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv, int n_kv_heads,
                       int group, int d_head, int n_cus, CrossList* out) {
   const Lengths s = {n_seqs, cu_q, cu_kv, group};
-  int64_t work = 0, longest = 0;
-  bool wide = false;
+  int64_t work = 0, longest = 0, units = 0;
   for (int64_t i = 0; i < n_seqs; ++i) {
     const int64_t rows = s.rows(i), kb = blocks32(s.keys(i));
     work += blocks32(rows) * kb * n_kv_heads;
+    units += (rows > 64 ? (rows + 127) / 128 : rows > 0) * n_kv_heads;
     if (rows > 0) longest = std::max(longest, kb);
-    wide = wide || rows > 32;
   }
   auto share = [&](int per_cu) {
     const int64_t waves = (int64_t)n_cus * per_cu;
-    return std::max<int64_t>(8, (work + waves - 1) / waves);
+    return std::max<int64_t>(2, (work + waves - 1) / waves);
   };
-  *out = split_list(s, share(4));
-  size_t units = 0;
-  for (const auto& items : out->items) units += items.size() * n_kv_heads;
-  if (!wide || longest <= share(8) || units > (size_t)n_cus * 8) return;
+  // Of many units only the longest matter: they are split where one alone
+  // would take a good part of the whole.
+  if (units > 8 * (int64_t)n_cus) {
+    *out = split_list(s, longest > share(4) ? std::max<int64_t>(16, share(4)) : longest);
+    return;
+  }
+  *out = split_list(s, std::max<int64_t>(longest, 1));
   double best = list_us(*out, n_kv_heads, d_head, n_cus);
-  for (int per_cu : {6, 8}) {
-    CrossList list = split_list(s, share(per_cu));
+  int64_t last = longest;
+  for (int per_cu : {4, 6, 8}) {
+    if (share(per_cu) >= last) continue;
+    last = share(per_cu);
+    CrossList list = split_list(s, last);
     const double us = list_us(list, n_kv_heads, d_head, n_cus);
     if (us < best) {
       best = us;

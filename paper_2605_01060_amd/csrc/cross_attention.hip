@@ -53,6 +53,14 @@ __device__ __forceinline__ int kv_copy_chunk(int lane, int copy) {
   return copy_chunk<4>(lane, copy);
 }
 
+// v combined with its value in lane ^ 32: an exchange in registers, where one
+// through LDS would be a latency of it in every block's chain.
+template <class Op>
+__device__ __forceinline__ float with_other_half(float v, Op op) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // WAVES waves of 32 rows against blocks of KB keys that they share in LDS, the
 // next block copied while the current one is on the MFMA units.
 template <int DH, int WAVES, int KB>
@@ -66,6 +74,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DH =
   constexpr uint64_t FULL = KB == 64 ? ~0ull : 0xffffffffull;
   static_assert((KB == 32 || KB == 64) && NCP >= 1, "a block is copied by whole instructions");
   __shared__ __attribute__((aligned(256))) u32x4 sKV[4 * BUF / 16];  // K blocks by parity, then V blocks
+  __shared__ f32x4 sBias[WAVES][16];  // what a wave adds to its scores: 0 or -inf by key
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % a.n_kv_heads;
@@ -105,12 +114,9 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DH =
     copy_block(kb, a.ld_k, i, (i & 1) * BUF);
     copy_block(vb, a.ld_v, i, (2 + (i & 1)) * BUF);
   };
-  // Key KB i + lane (% 32 of a 32-key block) is there and not masked.
-  auto key_on = [&](int i) {
-    const int key = i * KB + (lane & (KB - 1));
-    bool on = key < n_keys;
-    if (mask && on) on = mask[key] != 0;
-    return on;
+  // The mask's byte of key KB i + lane (% 32 of a 32-key block).
+  auto mask_byte = [&](int i) -> uint32_t {
+    return mask ? mask[min(i * KB + (lane & (KB - 1)), n_keys - 1)] : 1u;
   };
 
   // LDS addresses.  K: chunk 2 kk + half of row col; the swizzle is an
@@ -142,51 +148,73 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DH =
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
 
-  bool on = false;
+  // A block's mask is loaded a block ahead and looked at where it is used: a
+  // comparison at once would wait for the copies before it.
+  uint32_t byte = 0;
   if (n > 0) {
     copy_kv(0);
-    on = key_on(0);
+    byte = mask_byte(0);
   }
   for (int i = 0; i < n; ++i) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const bool on = byte != 0 && i * KB + (lane & (KB - 1)) < n_keys;
     const uint64_t keys = __ballot(on) & FULL;
     if (keys != FULL) {
-      // What stands in the V rows of absent keys must not reach the products.
+      // Absent keys: -inf in the accumulators that their scores start from, and
+      // zeros over what stands in their rows of K and V, where a NaN or an
+      // infinity would reach the products.
+      reinterpret_cast<float*>(sBias[wave])[lane] = on ? 0.0f : -INFINITY;
+      const uint32_t own = (uint32_t)(keys >> (wave * NCP * RPC));  // of the rows that this wave copied
+      u32x4* const k_rows = sKV + (i & 1) * (BUF / 16) + wave * (NCP * 64) + lane;
 #pragma unroll
       for (int j = 0; j < NCP; ++j)
-        if (!(keys >> ((wave * NCP + j) * RPC + lane / CPR) & 1))
-          sKV[(2 + (i & 1)) * (BUF / 16) + (wave * NCP + j) * 64 + lane] = u32x4{0u, 0u, 0u, 0u};
+        if (!(own >> (j * RPC + lane / CPR) & 1u)) {
+          k_rows[j * 64] = u32x4{0u, 0u, 0u, 0u};
+          k_rows[2 * (BUF / 16) + j * 64] = u32x4{0u, 0u, 0u, 0u};
+        }
     }
     __syncthreads();  // the block is there, the other one read out
     if (i + 1 < n) {
       copy_kv(i + 1);
-      on = key_on(i + 1);
+      byte = mask_byte(i + 1);
     }
     if (active && keys) {
       f32x16 s[T];
       // Ahead of the waves of the SIMD that are at their exponentials.
       __builtin_amdgcn_s_setprio(1);
+      auto step = [&](int t, int kk, const f32x16& c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], c, 0, 0, 0);
+      };
+      // (Two ways to the first step, so that the one without absent keys starts
+      // from the constant 0.)
+      if (keys == FULL) {
+        f32x16 zero;
 #pragma unroll
-      for (int t = 0; t < T; ++t)
+        for (int r = 0; r < 16; ++r) zero[r] = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+        for (int t = 0; t < T; ++t) s[t] = step(t, 0, zero);
+      } else {
 #pragma unroll
-      for (int kk = 0; kk < KSTEPS; ++kk)
+        for (int t = 0; t < T; ++t) {
+          f32x16 bias;
 #pragma unroll
-        for (int t = 0; t < T; ++t)
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
-      __builtin_amdgcn_s_setprio(0);
-      if (keys != FULL) {
+          for (int g = 0; g < 4; ++g) {
+            const f32x4 v = sBias[wave][t * 8 + 2 * g + half];
 #pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!(keys >> (32 * t + 8 * (r >> 2) + 4 * half + (r & 3)) & 1)) s[t][r] = -INFINITY;
+            for (int r = 0; r < 4; ++r) bias[4 * g + r] = v[r];
+          }
+          s[t] = step(t, 0, bias);
+        }
       }
+#pragma unroll
+      for (int kk = 1; kk < KSTEPS; ++kk)
+#pragma unroll
+        for (int t = 0; t < T; ++t) s[t] = step(t, kk, s[t]);
+      __builtin_amdgcn_s_setprio(0);
       float mloc = s[0][0];
 #pragma unroll
       for (int r = 1; r < 16 * T; ++r) mloc = fmaxf(mloc, s[r >> 4][r & 15]);
-      mloc = fmaxf(mloc, __shfl_xor(mloc, 32, 64)) * a.scale_log2;
+      mloc = with_other_half(mloc, [](float x, float y) { return fmaxf(x, y); }) * a.scale_log2;
       // The reference of the exponentials follows the maximum only where that
       // has grown by more than 2^8: the probabilities stay below 2^8.
       if (__any(mloc > m_ref + 8.0f)) {
@@ -217,7 +245,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DH =
     ka += other;
     va += other;
   }
-  l_run += __shfl_xor(l_run, 32, 64);
+  l_run = with_other_half(l_run, [](float x, float y) { return x + y; });
 
   // Register r of tile dt: feature dt 32 + 8 (r / 4) + 4 half + r % 4 of row col.
   if (item.part < 0) {
