@@ -116,13 +116,14 @@ double list_us(const CrossList& list, int n_kv_heads, int d_head, int n_cus) {
 // to 8 waves per CU would have of all of them, and at least two, or all keys
 // of its rows.  Few large units leave CUs idle at the end or wait for one
 // wave's chain of blocks, many cost the join, and which is less depends on the
-// lengths: the list with the least time by list_us is taken.  Measured (us, 4
-// / 6 / 8 waves per CU): heads 16 / 4 x 128, four texts of about 6000, 1500
-// queries each, 313 / 343 / 345; 16 x 64, 7 texts of about 5000, 300 queries,
-// 160 / 162 / 136; 12 x 64, two of about 9000, 2000 queries, 121 / 91 / 111.
-// One query over 512 keys, 12 x 64, shares of 2 / 4 / 8 blocks: 6.4 / 7.2 /
-// 9.6.  64 texts of about 96 keys, one query, 16 x 64: whole 9.6, shares of 4
-// blocks 12.0.
+// lengths: the list with the least time by list_us is taken.  Measured (us,
+// whole, then shares of 4 / 6 / 8 waves per CU): heads 16 / 4 x 128, four texts
+// of about 6000, 1500 queries each, 320, 322 / 338 / 335; 16 x 64, 7 texts of
+// about 5000, 300 queries, 161, 134 / 120 / 123; 12 x 64, two of about 9000,
+// 2000 queries, 134, 119 / 96 / 106; 16 x 64, three of about 20,000, one query,
+// 575, 49.8 / 53.3 / 56.0.  One query over 512 keys, 12 x 64: whole 12.5,
+// shares of 2 / 4 / 8 blocks 6.4 / 7.2 / 9.7; 64 texts of about 96 keys, one
+// query, 16 x 64: 8.7, of 2 / 4 blocks 13.0 / 11.7.
 void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv, int n_kv_heads,
                       int group, int d_head, int n_cus, CrossList* out) {
   const Lengths s = {n_seqs, cu_q, cu_kv, group};

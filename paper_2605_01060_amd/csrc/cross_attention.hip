@@ -10,14 +10,37 @@
 // (sequence, key head) is query r / G, head r % G of the group, so that a
 // step of one query with shared heads fills a tile as G queries would.
 //
-// A unit is 32 rows of one (sequence, key head) over a range of its keys.  A
-// wave computes S^T = K Q^T with 32x32x16 MFMAs, so that a lane owns one row
-// (running maximum, sum and rescaling are the lane's own, joined with lane ^
-// 32 that has the other half of a key block), keeps the probabilities in
-// registers as the operand of O^T += V^T P^T, and reads V^T from the
-// row-major V block with the transposing LDS read.  Where one (sequence, key
-// head)'s keys are split over units, each writes its maximum, sum and
-// unnormalised output in fp32, and a second kernel joins them in key order.
+// A unit is up to 128 rows of one (sequence, key head) over a range of its
+// keys, in waves of 32 rows that share blocks of keys in LDS.  A wave computes
+// S^T = K Q^T with 32x32x16 MFMAs, so that a lane owns one row (running
+// maximum, sum and rescaling are the lane's own, joined with lane ^ 32 that
+// has the other half of a key block), keeps the probabilities in registers as
+// the operand of O^T += V^T P^T, and reads V^T from the row-major V block with
+// the transposing LDS read.  The probabilities are rounded to bf16, the type
+// of V and of the MFMA; maxima, sums and outputs stay fp32.  Where one
+// (sequence, key head)'s keys are split over units, each writes its maximum,
+// sum and unnormalised output in fp32, and a second kernel joins them in key
+// order.
+//
+// Unit sizes: 128 rows against 64 keys (a key block is read from LDS once for
+// four waves' rows), 64 rows against 32 keys for sequences of 33 to 64 rows
+// (2000 texts of 64 keys, 64 queries, 12 x 64: 225 us as half-empty units of
+// 128, 187 so) and one wave of 32 rows against 32 keys, with the most waves
+// per CU, for fewer (a stream of keys).
+//
+// What bounds it, measured: many rows, the power limit and the exponentials.
+// 8 sequences, 2048 queries, 8192 keys, 16 heads x 128 take 1,060 us, 1,040
+// TFLOP/s, at 1.76 GHz with the MFMA pipe 46 % busy; 16 x 64 (4096 queries)
+// 951 TFLOP/s, 16 x 32 687, where a score costs the VALU the same and the MFMAs
+// a half and a quarter.  Few rows, memory: one query of 32 / 8 heads x 128 over
+// 100,003 keys streams them in 74 us, 5.5 TB/s, and joins in 6.  Small calls, a
+// wave's chain: about 0.6 us per block of 32 keys (MFMA and LDS latencies; a
+// deeper ring of blocks changes nothing).
+//
+// Tried and dropped: K a block ahead of V, so that the scores of the next block
+// run under the exponentials of this one (48 spilled registers at d_head 128,
+// 410 -> 523 us); the sum of the rounded probabilities by dot products (-1 to
+// -2 %); four waves per SIMD at d_head 32 (16 spilled, 189 -> 242 us).
 #include <math.h>
 
 #include <algorithm>

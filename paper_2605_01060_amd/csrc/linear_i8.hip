@@ -7,6 +7,25 @@
 // A row's 128 bytes of a K stage are laid out as the bf16 layers lay out
 // their 64 values: a fragment of a 16x16x64 MFMA is 16 rows x four 16-byte
 // chunks, read from LDS rows whose chunk c of row r sits at c ^ (r & 7).
+//
+// Three kinds of kernel, chosen by a model of their times (below): persistent
+// 256 x 256 and 192 x 256 tiles with the schedule of linear_wide.hip, rings of
+// one tile per workgroup for launches of few tiles, and a kernel for few
+// tokens.
+//
+// What bounds them, measured: large K, the power limit (8192^3 in 380 us, 2,892
+// TOP/s; M = 200,003, N = 1024, K = 4096 with residual 735 us, 2,280); K = 768, the
+// epilogue, during which a CU's MFMA pipe idles (M = 200,003, N = 2304: 393 us,
+// 1,800 TOP/s at 2.0 GHz, MFMA pipe 45 % busy, VALU 26 %); few tiles, a tile's
+// chain of K stages (0.26 us each); one token, 2.7 us, the latencies of a launch,
+// two loads and a meeting of eight waves.
+//
+// Tried and dropped: starting the CUs apart, so that their stores do not come
+// at once (it costs its delay and gains nothing); the channel vectors in
+// registers over the epilogue's passes (+-1 %); two workgroups of 128 x 256
+// tiles on a CU, one's epilogue under the other's MFMAs (M = 200,003, N = 2304, K =
+// 768 406 -> 487 us: two thirds of the MFMAs per copied byte);
+// ordinary instead of nontemporal output stores (400 -> 416 us).
 #include <algorithm>
 
 #include "linear_common.h"
