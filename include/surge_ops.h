@@ -237,7 +237,7 @@ surge_status surge_cross_plan_info(const surge_cross_plan* plan, int64_t* worksp
  * d_q, d_out bf16 [cu_q[n], n_heads d_head]; d_k, d_v bf16 [cu_kv[n],
  * n_kv_heads d_head] (two column ranges of one projection's output, say, with
  * its stride); d_key_mask one byte per state, 0 leaves it out (what stands in
- * its rows of k and v does not matter), or NULL; scale positive and finite.
+ * its rows of k and v does not matter), or NULL; scale positive, below 2^127.
  * d_workspace: 16-byte aligned, of at least the plan's bytes (NULL where
  * that is 0), used until the call's work is done: calls that may run at the
  * same time, graph replays among them, need one each.  d_out must not

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <exception>
 #include <new>
 
 #include "cross.h"
@@ -55,6 +56,14 @@ surge_status check_vector(const char* name, const void* p, bool needed) {
   if (!p && needed) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s is NULL", name);
   if (!aligned(p, 16)) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s must be 16-byte aligned", name);
   return SURGE_OK;
+}
+
+// An output in the place of an input (`over` says whether it may be, with the
+// same stride) or of another output.
+surge_status check_place(const char* name, const void* p, int64_t ld, const char* other, const void* q,
+                         int64_t ld_other, bool over) {
+  if (!p || p != q || (over && ld == ld_other)) return SURGE_OK;
+  return fail(SURGE_ERR_INVALID_ARGUMENT, over ? "%s over %s needs its stride" : "%s is %s", name, other);
 }
 
 surge_status check_rows(int64_t M) {
@@ -125,6 +134,7 @@ surge_status surge_op_quantize_rows(int64_t M, int32_t K, const uint16_t* d_x, i
   CHECK(check_matrix("x", d_x, K, ld_x, 8));
   CHECK(check_matrix("q", d_q, i8_columns(K), ld_q, 16));
   if (!d_scale) return fail(SURGE_ERR_INVALID_ARGUMENT, "scale is NULL");
+  CHECK(check_place("q", d_q, 0, "x", d_x, 0, false));
   int dev = 0, n_cus = 0;
   CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   HIP_TRY(launch_quantize_rows(M, K, d_x, ld_x, d_q, ld_q, d_scale, (hipStream_t)hip_stream));
@@ -151,6 +161,9 @@ surge_status surge_op_linear_i8(int64_t M, int32_t N, int32_t K, const int8_t* d
   CHECK(check_vector("w", d_w, true));
   CHECK(check_vector("w_scale", d_w_scale, true));
   CHECK(check_vector("bias", d_bias, true));
+  CHECK(check_place("y", d_y, 0, "x", d_x, 0, false));
+  CHECK(check_place("y", d_y, 0, "w", d_w, 0, false));
+  if (epilogue == 2) CHECK(check_place("y", d_y, ld_y, "res", d_res, ld_res, true));
   int dev = 0, n_cus = 0;
   CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   const LinearI8 a = {d_x,    d_w,    ld_x, d_x_scale, d_w_scale, d_bias,
@@ -206,6 +219,19 @@ surge_status surge_op_block_norm(int64_t M, int32_t d, int32_t kind, const uint1
   CHECK(check_vector("gate", d_gate, false));
   CHECK(check_vector("pre_gamma", d_pre_gamma, norm));
   CHECK(check_vector("pre_beta", d_pre_beta, false));
+  const struct {
+    const char* name;
+    const void* p;
+    int64_t ld;
+  } ins[] = {{"x", d_x, ld_x}, {"block", d_block, ld_block}, {"gate_rows", d_gate_rows, ld_gate}};
+  for (const auto& in : ins) {
+    CHECK(check_place("y", d_y, ld_y, in.name, in.p, in.ld, true));
+    CHECK(check_place("z", d_z, ld_z, in.name, in.p, in.ld, true));
+    CHECK(check_place("zq", d_zq, 0, in.name, in.p, 0, false));
+  }
+  CHECK(check_place("z", d_z, 0, "y", d_y, 0, false));
+  CHECK(check_place("zq", d_zq, 0, "y", d_y, 0, false));
+  CHECK(check_place("zq", d_zq, 0, "z", d_z, 0, false));
   const BlockNorm a = {d_x,         d_block,    d_gate_rows, ld_x, ld_block, ld_gate, d_post_gamma,
                        d_post_beta, d_gate,     d_pre_gamma, d_pre_beta, res_scale, eps, d_y, d_z,
                        ld_y,        ld_z,       d_zq,        ld_zq, d_zq_scale};
@@ -277,6 +303,8 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     *out = p;
   } catch (const std::bad_alloc&) {
     return fail(SURGE_ERR_OUT_OF_MEMORY, "host memory for the plan");
+  } catch (const std::exception& e) {
+    return fail(SURGE_ERR_INTERNAL, "the plan's list: %s", e.what());
   }
   return SURGE_OK;
 }
@@ -310,8 +338,10 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
                                       int64_t ld_out, void* hip_stream) {
   clear_error();
   if (!plan) return fail(SURGE_ERR_INVALID_ARGUMENT, "plan is NULL");
-  if (!(scale > 0.0f) || !isfinite(scale))
-    return fail(SURGE_ERR_INVALID_ARGUMENT, "scale=%g must be positive and finite", (double)scale);
+  // Times log2(e) it is still a float.
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if (!(scale > 0.0f) || !isfinite(scale_log2))
+    return fail(SURGE_ERR_INVALID_ARGUMENT, "scale=%g must be positive and below 2^127", (double)scale);
   if (plan->n_units == 0) return SURGE_OK;
   const int64_t kv_cols = (int64_t)plan->n_kv_heads * plan->d_head;
   const int64_t cols = kv_cols * plan->group;
@@ -343,7 +373,7 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
   a.ld_k = ld_k;
   a.ld_v = ld_v;
   a.mask = d_key_mask;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale_log2;
   a.n_kv_heads = plan->n_kv_heads;
   a.group = plan->group;
   a.items = (const CrossItem*)plan->lists;

@@ -647,6 +647,7 @@ def test_cross_attention_refusals_with_a_plan():
     good = dict(plan=plan, d_q=p["q"], ld_q=128, d_k=p["kv"], ld_k=256, d_v=p["kv"][:, 128:], ld_v=256,
                 key_mask=None, scale=0.125, workspace=ws, d_out=out, ld_out=128)
     for change in (dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf),
+                   dict(scale=3e38), dict(d_out=p["kv"], ld_out=256),
                    dict(workspace=None), dict(workspace=ws[16:]), dict(d_q=None), dict(d_k=None),
                    dict(d_v=None), dict(d_out=None), dict(ld_q=120), dict(ld_k=132), dict(ld_v=64),
                    dict(ld_out=1 << 23), dict(d_out=p["q"]), dict(d_q=p["q"].data_ptr() + 2)):

@@ -7,7 +7,8 @@ import pytest
 
 from paper_2605_01060_amd import surge as S
 
-A = 1 << 20  # a 16-byte aligned address
+A = 1 << 20  # 16-byte aligned addresses
+X, Y, Z, Q, R = (A + (i << 12) for i in range(1, 6))
 NAN, INF = float("nan"), float("inf")
 
 
@@ -18,20 +19,20 @@ def refused(fn, args, **change):
     return e.value
 
 
-QUANT = dict(M=3, K=200, d_x=A, ld_x=200, d_q=A, ld_q=256, d_scale=A)
+QUANT = dict(M=3, K=200, d_x=X, ld_x=200, d_q=Q, ld_q=256, d_scale=A)
 
 
 @pytest.mark.parametrize("change", [
     dict(M=-1), dict(M=1 << 31), dict(K=0), dict(K=12), dict(K=16392, ld_x=16392, ld_q=16512),
     dict(d_x=0), dict(d_q=0), dict(d_scale=0), dict(d_x=A + 8), dict(d_q=A + 8), dict(ld_x=192),
-    dict(ld_x=204), dict(ld_q=208), dict(ld_q=264), dict(ld_x=(1 << 22) + 8),
+    dict(ld_x=204), dict(ld_q=208), dict(ld_q=264), dict(ld_x=(1 << 22) + 8), dict(d_q=X),
 ])
 def test_quantize_rows_refuses(change):
     refused(S.surge_op_quantize_rows, QUANT, **change)
 
 
-LINEAR = dict(M=3, N=24, K=128, d_x=A, ld_x=128, d_x_scale=A, d_w=A, d_w_scale=A, d_bias=A, d_res=A,
-              ld_res=24, epilogue=2, d_y=A, ld_y=24)
+LINEAR = dict(M=3, N=24, K=128, d_x=X, ld_x=128, d_x_scale=A, d_w=A, d_w_scale=A, d_bias=A, d_res=R,
+              ld_res=24, epilogue=2, d_y=Y, ld_y=24)
 
 
 @pytest.mark.parametrize("change", [
@@ -41,14 +42,15 @@ LINEAR = dict(M=3, N=24, K=128, d_x=A, ld_x=128, d_x_scale=A, d_w=A, d_w_scale=A
     dict(d_bias=0), dict(d_res=0), dict(d_y=0), dict(d_x=A + 4), dict(d_w=A + 8),
     dict(d_w_scale=A + 4), dict(d_bias=A + 8), dict(d_res=A + 2), dict(d_y=A + 8), dict(ld_x=112),
     dict(ld_x=136), dict(ld_y=16), dict(ld_y=28), dict(ld_res=16), dict(ld_x=1 << 23),
+    dict(d_y=X), dict(d_y=A), dict(d_y=R, ld_y=32),
 ])
 def test_linear_i8_refuses(change):
     refused(S.surge_op_linear_i8, LINEAR, **change)
 
 
-NORM = dict(M=3, d=200, kind=S.NORM_LAYER, d_x=A, ld_x=200, d_block=A, ld_block=200, post_gamma=A,
+NORM = dict(M=3, d=200, kind=S.NORM_LAYER, d_x=X, ld_x=200, d_block=R, ld_block=200, post_gamma=A,
             post_beta=A, gate=A, gate_rows=A, ld_gate=200, res_scale=1.0, pre_gamma=A, pre_beta=A,
-            eps=1e-5, d_y=A, ld_y=200, d_z=A, ld_z=200, d_zq=A, ld_zq=256, zq_scale=A)
+            eps=1e-5, d_y=Y, ld_y=200, d_z=Z, ld_z=200, d_zq=Q, ld_zq=256, zq_scale=A)
 
 
 @pytest.mark.parametrize("change", [
@@ -63,6 +65,8 @@ NORM = dict(M=3, d=200, kind=S.NORM_LAYER, d_x=A, ld_x=200, d_block=A, ld_block=
     dict(post_gamma=A + 4), dict(post_beta=A + 4), dict(pre_gamma=A + 4), dict(pre_beta=A + 4),
     dict(d_y=A + 8), dict(d_z=A + 8), dict(d_zq=A + 8), dict(ld_x=192), dict(ld_block=196),
     dict(ld_gate=100), dict(ld_y=192), dict(ld_z=204), dict(ld_zq=208),
+    dict(d_z=Y), dict(d_zq=Y), dict(d_zq=Z), dict(d_zq=X), dict(d_zq=A), dict(d_y=X, ld_y=208),
+    dict(d_z=R, ld_z=208), dict(d_y=A, ld_gate=208),
 ])
 def test_block_norm_refuses(change):
     refused(S.surge_op_block_norm, NORM, **change)
