@@ -148,11 +148,7 @@ def _host(a: np.ndarray, dtype) -> Tuple[np.ndarray, int]:
 
 
 def _dev(x) -> int:
-    if x is None:
-        return 0
-    if isinstance(x, int):
-        return x
-    return int(x.data_ptr())
+    return 0 if x is None else x if isinstance(x, int) else x.data_ptr()
 
 
 def _hptr(x) -> int:
@@ -169,11 +165,7 @@ def _hptr(x) -> int:
 
 
 def _stream(s) -> Optional[int]:
-    if s is None:
-        return None
-    if isinstance(s, int):
-        return s
-    return int(s.cuda_stream)
+    return s if s is None or isinstance(s, int) else s.cuda_stream
 
 
 def surge_version() -> str:
