@@ -56,7 +56,7 @@ __device__ __forceinline__ i32x4 mma(i32x4 w, i32x4 x, i32x4 c) {
 // loaded ahead, whole 128-byte row segments stored.  slot16(r, c): 16-byte
 // slot c of region row r.  vec(v, q): the scales (v = 0) or biases (1) of the
 // wave's channels 4 q .. 4 q + 3.  scale(r): the scale of the wave's row r.
-template <int TJ, int TI, int EPI, bool RAGGED_N, class Slot, class Vec, class Scale>
+template <int TJ, int TI, int EPI, class Slot, class Vec, class Scale>
 __device__ __forceinline__ void store_i8(const i32x4 (&acc)[TI][TJ], Slot slot16, Vec vec, Scale scale,
                                          const LinearI8& a, int mw, int nw, int M, int N, int lane) {
   constexpr bool RES = EPI == EPI_BIAS_RESIDUAL;
@@ -66,7 +66,6 @@ __device__ __forceinline__ void store_i8(const i32x4 (&acc)[TI][TJ], Slot slot16
   const int l16 = lane & 15, lq = lane >> 4;
   const int cr = lane >> 3;  // row within the 8 rows of one coalesced access
   const int cp = lane & 7;   // 16-byte pair within a row
-  const uint32_t to = (uint32_t)cr * (uint32_t)a.ld_y * 2u + (uint32_t)cp * 16u;
   u32x4 rv[RES ? NP : 1][4];
   if constexpr (RES) {
 #pragma unroll
@@ -74,9 +73,9 @@ __device__ __forceinline__ void store_i8(const i32x4 (&acc)[TI][TJ], Slot slot16
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
         const int m = min(mw + p / PI * 32 + it * 8 + cr, M - 1);
-        const int n = nw + p % PI * 64 + 8 * cp;
+        const int n = min(nw + p % PI * 64 + 8 * cp, N - 8);
         rv[p][it] = __builtin_nontemporal_load(
-            reinterpret_cast<const u32x4*>(a.res + (int64_t)m * a.ld_res + (RAGGED_N ? min(n, N - 8) : n)));
+            reinterpret_cast<const u32x4*>(a.res + (int64_t)m * a.ld_res + n));
       }
   }
 #pragma unroll
@@ -119,14 +118,12 @@ __device__ __forceinline__ void store_i8(const i32x4 (&acc)[TI][TJ], Slot slot16
     // Everything issued before the tile's first store is done by here: the
     // copies in flight retire before the stores and need not wait for them.
     if (p == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    // (From a scalar address and one offset a lane.)
-    uint16_t* const y0 = a.y + (int64_t)(mw + j * 32) * a.ld_y + (nw + ip * 64);
-    const bool in_n = !RAGGED_N || nw + ip * 64 + 8 * cp < N;
 #pragma unroll
-    for (int it = 0; it < 4; ++it)
-      if (mw + j * 32 + it * 8 + cr < M && in_n)
-        __builtin_nontemporal_store(
-            ov[it], reinterpret_cast<u32x4*>(reinterpret_cast<char*>(y0 + (int64_t)it * 8 * a.ld_y) + to));
+    for (int it = 0; it < 4; ++it) {
+      const int m = mw + j * 32 + it * 8 + cr, n = nw + ip * 64 + 8 * cp;
+      if (m < M && n < N)
+        __builtin_nontemporal_store(ov[it], reinterpret_cast<u32x4*>(a.y + (int64_t)m * a.ld_y + n));
+    }
   }
 }
 
@@ -363,7 +360,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void l
     };
     auto vec = [&](int v, int q) { return svec[tpar][v][(wn0 >> 2) + q]; };
     auto scale = [&](int r) { return srow[tpar][wm0 + r]; };
-    store_i8<TJ, TI, EPI, false>(acc, slot16, vec, scale, a, m0 + wm0, n0 + wn0, M, 0, opaque_lane());
+    store_i8<TJ, TI, EPI>(acc, slot16, vec, scale, a, m0 + wm0, n0 + wn0, M, INT32_MAX, opaque_lane());
 
     // The held-back copies, into slots only this wave has used since.
     const uint32_t go = more();
@@ -467,7 +464,7 @@ linear_i8_ring_kernel(LinearI8 a, int M, int N, int K, int tiles_n, int n_tiles)
     return *reinterpret_cast<const float4*>((v ? a.bias : a.w_scale) + n);
   };
   auto scale = [&](int r) { return a.x_scale[min(m0 + wm0 + r, M - 1)]; };
-  store_i8<TJ, TI, EPI, true>(acc, slot16, vec, scale, a, m0 + wm0, n0 + wn0, M, N, lane);
+  store_i8<TJ, TI, EPI>(acc, slot16, vec, scale, a, m0 + wm0, n0 + wn0, M, N, lane);
 }
 
 // A few tokens: the launch's time is a wave's chain and the stream of W.  16
