@@ -68,45 +68,55 @@ struct UnitCost {
   int places;
   double base, chain, full;
 };
-const UnitCost& unit_cost(int cls, int d_head) {
+UnitCost unit_cost(int cls, int d_head, bool short_blocks) {
   static const UnitCost costs[CROSS_CLASSES][3] = {
       {{5, 2.9, 0.31, 0.98}, {4, 3.2, 0.47, 1.13}, {2, 4.3, 0.60, 1.03}},
       {{14, 2.6, 0.47, 0.47}, {8, 3.0, 0.58, 0.58}, {4, 3.7, 0.80, 0.80}},
       {{19, 2.4, 0.46, 0.46}, {9, 2.5, 0.62, 0.62}, {4, 2.9, 0.94, 0.94}},
   };
+  if (short_blocks) return {3, 4.0, 0.80, 1.47};
   return costs[cls][d_head / 64];
 }
 
-// What a list takes, in us: each class as its units, longest first, go to the
-// first free of the chip's places, or as its keys come from memory, then the
-// join.
-double list_us(const CrossList& list, int n_kv_heads, int d_head, int n_cus) {
-  double us = 0;
-  for (int c = 0; c < CROSS_CLASSES; ++c) {
-    const int64_t units = (int64_t)list.items[c].size() * n_kv_heads;
-    if (units == 0) continue;
-    const UnitCost& q = unit_cost(c, d_head);
-    const double load = std::min(1.0, (double)units / ((double)n_cus * q.places));
-    const double block = std::max(q.chain, q.full * load);
-    std::priority_queue<double, std::vector<double>, std::greater<double>> places;
-    double end = 0, keys = 0;
-    for (const CrossItem& it : list.items[c]) {
-      keys += it.k1 - it.k0;
-      for (int h = 0; h < n_kv_heads; ++h) {
-        double t = q.base + (double)blocks32(it.k1 - it.k0) * block;
-        if ((int)places.size() == q.places * n_cus) {
-          t += places.top();
-          places.pop();
-        }
-        places.push(t);
-        end = std::max(end, t);
+// What the units of a class take, in us: longest first they go to the first
+// free of the chip's places, or their keys come from memory.
+double class_us(const CrossList& list, int cls, int n_kv_heads, int d_head, bool short_blocks, int n_cus) {
+  const int64_t units = (int64_t)list.items[cls].size() * n_kv_heads;
+  if (units == 0) return 0;
+  const UnitCost q = unit_cost(cls, d_head, short_blocks);
+  const double load = std::min(1.0, (double)units / ((double)n_cus * q.places));
+  const double block = std::max(q.chain, q.full * load);
+  std::priority_queue<double, std::vector<double>, std::greater<double>> places;
+  double end = 0, keys = 0;
+  for (const CrossItem& it : list.items[cls]) {
+    keys += it.k1 - it.k0;
+    for (int h = 0; h < n_kv_heads; ++h) {
+      double t = q.base + (double)blocks32(it.k1 - it.k0) * block;
+      if ((int)places.size() == q.places * n_cus) {
+        t += places.top();
+        places.pop();
       }
+      places.push(t);
+      end = std::max(end, t);
     }
-    if (c > 0) end = std::max(end, q.base + keys * n_kv_heads * d_head * 4 / 4.9e6);
-    us += end;
   }
-  if (list.n_parts > 0)
-    us += 2.7 + (double)list.n_parts * n_kv_heads * 32 * (d_head * 8 + 16) / 4e6;
+  if (cls > 0) end = std::max(end, q.base + keys * n_kv_heads * d_head * 4 / 4.9e6);
+  return end;
+}
+
+// What a list takes, with the better of the two blocks for units of 128 rows
+// of 128-dimensional heads, and the join.
+double list_us(CrossList* list, int n_kv_heads, int d_head, int n_cus) {
+  double us = class_us(*list, 0, n_kv_heads, d_head, false, n_cus);
+  list->short_blocks = false;
+  if (d_head == 128) {
+    const double other = class_us(*list, 0, n_kv_heads, d_head, true, n_cus);
+    list->short_blocks = other < us;
+    us = std::min(us, other);
+  }
+  for (int c = 1; c < CROSS_CLASSES; ++c) us += class_us(*list, c, n_kv_heads, d_head, false, n_cus);
+  if (list->n_parts > 0)
+    us += 2.7 + (double)list->n_parts * n_kv_heads * 32 * (d_head * 8 + 16) / 4e6;
   return us;
 }
 
@@ -139,19 +149,23 @@ void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv,
     return std::max<int64_t>(2, (work + waves - 1) / waves);
   };
   // Of many units only the longest matter: they are split where one alone
-  // would take a good part of the whole.
+  // would take a good part of the whole.  Blocks of 32 and of 64 keys are within
+  // 1 % of each other there but for the shortest texts (500 sequences, 128
+  // queries, 192 / 288 keys, 8 heads x 128: 64 keys 124 / 165, 32 keys 125 / 163
+  // us) and for lengths that differ (60, 300, about 1500: 166 / 161).
   if (units > 8 * (int64_t)n_cus) {
     *out = split_list(s, longest > share(4) ? std::max<int64_t>(16, share(4)) : longest);
+    out->short_blocks = d_head == 128 && longest > 8;
     return;
   }
   *out = split_list(s, std::max<int64_t>(longest, 1));
-  double best = list_us(*out, n_kv_heads, d_head, n_cus);
+  double best = list_us(out, n_kv_heads, d_head, n_cus);
   int64_t last = longest;
   for (int per_cu : {4, 6, 8}) {
     if (share(per_cu) >= last) continue;
     last = share(per_cu);
     CrossList list = split_list(s, last);
-    const double us = list_us(list, n_kv_heads, d_head, n_cus);
+    const double us = list_us(&list, n_kv_heads, d_head, n_cus);
     if (us < best) {
       best = us;
       *out = std::move(list);

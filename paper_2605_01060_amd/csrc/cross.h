@@ -18,6 +18,7 @@ struct CrossAttention {
   int n_items[CROSS_CLASSES];
   const CrossJoin* joins;
   int n_joins, max_parts;
+  bool short_blocks;  // 128 rows of 128-dimensional heads against 32 keys
   float2* part_ml;  // [part, key head, 32] (maximum in log2 units, sum)
   float* part_o;    // [part, key head, 32, d_head]
   uint16_t* out;

@@ -28,11 +28,20 @@
 // 128, 187 so) and one wave of 32 rows against 32 keys, with the most waves
 // per CU, for fewer (a stream of keys).
 //
+// At d_head 128 the registers of 128 rows against 64 keys let a CU have two such
+// units, against 32 keys three, whose exponentials cover more of the others'
+// MFMAs; a block of 64 keys is the shorter chain.  The plan takes 32 where units
+// fill the third place (measured, 64 / 32 keys, us: 6 sequences, 500 queries,
+// about 10,000 keys, 16 / 4 heads 450 / 398; 4, 1500, 6000 with a mask
+// 328 / 309) and 64 where they don't (10 sequences, 300, about 2000, 8 heads
+// 48 / 53; 1, 1000, 1000, 16 / 4 24 / 28) or have few blocks (1000, 128, 128, 8
+// heads 192 / 197).
+//
 // What bounds it, measured: many rows, the power limit and the exponentials.
-// 8 sequences, 2048 queries, 8192 keys, 16 heads x 128 take 1,060 us, 1,040
-// TFLOP/s, at 1.76 GHz with the MFMA pipe 46 % busy; 16 x 64 (4096 queries)
-// 951 TFLOP/s, 16 x 32 687, where a score costs the VALU the same and the MFMAs
-// a half and a quarter.  Few rows, memory: one query of 32 / 8 heads x 128 over
+// 8 sequences, 2048 queries, 8192 keys, 16 heads x 128 take 1,010 to 1,060 us,
+// 1,040 to 1,090 TFLOP/s, at 1.8 GHz with the MFMA pipe half busy; 16 x 64 (4096
+// queries) 951 TFLOP/s, 16 x 32 687, where a score costs the VALU the same and
+// the MFMAs a half and a quarter.  Few rows, memory: one query of 32 / 8 heads x 128 over
 // 100,003 keys streams them in 74 us, 5.5 TB/s, and joins in 6.  Small calls, a
 // wave's chain: about 0.6 us per block of 32 keys (MFMA and LDS latencies; a
 // deeper ring of blocks changes nothing).
@@ -87,7 +96,8 @@ __device__ __forceinline__ float with_other_half(float v, Op op) {
 // WAVES waves of 32 rows against blocks of KB keys that they share in LDS, the
 // next block copied while the current one is on the MFMA units.
 template <int DH, int WAVES, int KB>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(DH == 128 ? 2 : 3))) void cross_kernel(
+__global__ __launch_bounds__(64 * WAVES)
+__attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_kernel(
     CrossAttention a, const CrossItem* items) {
   constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8;
   constexpr int RPC = 64 / CPR;          // rows that a copy instruction fills
@@ -389,15 +399,16 @@ template <int DH>
 hipError_t launch(const CrossAttention& a, hipStream_t stream) {
   const unsigned h = (unsigned)a.n_kv_heads;
   const CrossItem* items = a.items;
-#define SURGE_LAUNCH(CLASS, WAVES, KB)                                                            \
-  if (a.n_items[CLASS] > 0) {                                                                     \
-    hipLaunchKernelGGL((cross_kernel<DH, WAVES, KB>), dim3(a.n_items[CLASS] * h), dim3(64 * WAVES), \
-                       0, stream, a, items);                                                      \
-    items += a.n_items[CLASS];                                                                    \
-  }
-  SURGE_LAUNCH(0, 4, 64)
-  SURGE_LAUNCH(1, 2, 32)
-  SURGE_LAUNCH(2, 1, 32)
+#define SURGE_LAUNCH(CLASS, WAVES, KB)                                                               \
+  hipLaunchKernelGGL((cross_kernel<DH, WAVES, KB>), dim3(a.n_items[CLASS] * h), dim3(64 * WAVES), 0, \
+                     stream, a, items)
+  constexpr int SHORT = DH == 128 ? 32 : 64;  // the plan takes short blocks for DH 128 alone
+  if (a.n_items[0] > 0 && a.short_blocks) SURGE_LAUNCH(0, 4, SHORT);
+  if (a.n_items[0] > 0 && !a.short_blocks) SURGE_LAUNCH(0, 4, 64);
+  items += a.n_items[0];
+  if (a.n_items[1] > 0) SURGE_LAUNCH(1, 2, 32);
+  items += a.n_items[1];
+  if (a.n_items[2] > 0) SURGE_LAUNCH(2, 1, 32);
 #undef SURGE_LAUNCH
   const unsigned rows = (unsigned)a.n_joins * 32;
   if (a.n_joins > 0 && a.max_parts > 64)

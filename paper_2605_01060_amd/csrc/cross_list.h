@@ -35,6 +35,7 @@ struct CrossList {
   std::vector<CrossJoin> joins;
   int64_t n_parts = 0;                  // slots
   int max_parts = 0;                    // of one join
+  bool short_blocks = false;            // 128 rows against 32 keys, not 64
 };
 // cu_q, cu_kv: checked.  n_cus: compute units to fill.
 void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv, int n_kv_heads,

@@ -29,6 +29,7 @@ struct surge_cross_plan {
   int64_t q_tokens = 0, kv_tokens = 0;
   int n_items[CROSS_CLASSES] = {}, n_units = 0, n_joins = 0, max_parts = 0;
   int64_t n_parts = 0;
+  bool short_blocks = false;
   void* lists = nullptr;  // device: the items of each class, then the joins
 };
 
@@ -284,6 +285,7 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     p->n_joins = (int)list.joins.size();
     p->max_parts = list.max_parts;
     p->n_parts = list.n_parts;
+    p->short_blocks = list.short_blocks;
     const size_t bytes = items * sizeof(CrossItem) + list.joins.size() * sizeof(CrossJoin);
     p->device = dev;
     hipError_t e = hipSuccess;
@@ -381,6 +383,7 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
   a.joins = (const CrossJoin*)(a.items + plan->n_units);
   a.n_joins = plan->n_joins;
   a.max_parts = plan->max_parts;
+  a.short_blocks = plan->short_blocks;
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)((float*)d_workspace + part_rows(plan) * plan->d_head);
   a.out = d_out;

@@ -85,6 +85,7 @@ extern "C" void build(int64_t n, const int64_t* q, const int64_t* kv, int h, int
   sizes[4] = list.n_parts;
   sizes[5] = list.max_parts;
 }
+extern "C" int short_blocks() { return list.short_blocks; }
 extern "C" const void* items(int c) { return list.items[c].data(); }
 extern "C" const void* joins() { return list.joins.data(); }
 """
@@ -116,6 +117,7 @@ def lists(tmp_path_factory):
         return [array(lib.items(c), int(sizes[c]), 8) for c in range(3)], \
             array(lib.joins(), int(sizes[3]), 6), int(sizes[4]), int(sizes[5]), cu
 
+    build.short_blocks = lambda: bool(lib.short_blocks())
     return build
 
 
@@ -173,3 +175,17 @@ def test_few_rows_over_a_long_text_are_split_over_the_chip(lists):
     assert n_parts == max_parts == len(items[2]) and 4 * 256 * 0.9 <= 8 * n_parts <= 4 * 256
     items, joins, n_parts, _, _ = lists([1] * 2000, [48] * 2000, 12, 1, 64, 256)
     assert n_parts == 0 and len(joins) == 0 and len(items[2]) == 2000
+
+
+def test_short_blocks_of_keys_where_the_third_unit_of_a_cu_is_filled(lists):
+    def short(n, q, kv, heads, dh):
+        lists([q] * n, [kv] * n, heads, 1, dh, 256)
+        return lists.short_blocks()
+
+    assert short(96, 128, 1000, 8, 128)       # 768 units: 3 a CU
+    assert not short(128, 128, 1000, 8, 128)  # 1024: twice 2 a CU
+    assert not short(1, 128, 256, 12, 128)
+    assert short(300, 128, 512, 8, 128)       # many units
+    assert not short(300, 128, 256, 8, 128)   # of few blocks
+    for dh in (32, 64):
+        assert not short(96, 128, 1000, 8, dh) and not short(300, 128, 512, 8, dh)

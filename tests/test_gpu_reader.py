@@ -579,6 +579,22 @@ def test_cross_attention_over_long_texts(q, kv, heads, kv_heads, dh, mask):
     within(out, ref, tol)
 
 
+# The chip full of units of 128 rows: their blocks are of 32 keys at d_head 128.
+@pytest.mark.parametrize("seqs,q,kv,heads,kv_heads,dh", [(96, 128, 300, 8, 8, 128), (48, 60, 333, 32, 8, 128),
+                                                         (300, 97, 290, 8, 8, 128), (300, 70, 260, 8, 8, 64)])
+@pytest.mark.parametrize("mask", [None, 0.4])
+def test_cross_attention_on_a_full_chip(seqs, q, kv, heads, kv_heads, dh, mask):
+    torch = torch_cuda()
+    q_lengths = [q - i % 7 for i in range(seqs)]
+    kv_lengths = [0 if i == 5 else kv - (i * 37) % (kv // 2) for i in range(seqs)]
+    p = cross_inputs(q_lengths, kv_lengths, heads, kv_heads, dh, seqs + kv, mask)
+    out = torch.full((sum(q_lengths) + 1, heads * dh), math.nan, dtype=torch.bfloat16, device="cuda")
+    cross_call(p, out)
+    ref, tol = cross_reference(p)
+    within(out[:-1], ref, tol)
+    assert out[-1].isnan().all()
+
+
 def test_cross_attention_long_and_short_texts_together():
     torch = torch_cuda()
     kv = [3, 9000, 0, 17, 40_000, 1, 64, 2500]
