@@ -129,12 +129,13 @@ double list_us(CrossList* list, int n_kv_heads, int d_head, int n_cus) {
 // wave's chain of blocks, many cost the join, and which is less depends on the
 // lengths: the list with the least time by list_us is taken.  Measured (us,
 // whole, then shares of 4 / 6 / 8 waves per CU): heads 16 / 4 x 128, four texts
-// of about 6000, 1500 queries each, 320, 322 / 338 / 335; 16 x 64, 7 texts of
-// about 5000, 300 queries, 161, 134 / 120 / 123; 12 x 64, two of about 9000,
-// 2000 queries, 134, 119 / 96 / 106; 16 x 64, three of about 20,000, one query,
-// 575, 49.8 / 53.3 / 56.0.  One query over 512 keys, 12 x 64: whole 12.5,
-// shares of 2 / 4 / 8 blocks 6.4 / 7.2 / 9.7; 64 texts of about 96 keys, one
-// query, 16 x 64: 8.7, of 2 / 4 blocks 13.0 / 11.7.
+// of about 6000, 1500 queries each, 300, 300 / 322 / 290; 16 x 64, 7 texts of
+// about 5000, 300 queries, 160, 129 / 113 / 119; 12 x 64, two of about 9000,
+// 2000 queries, 134, 119 / 91 / 100; over 12 such calls and shares of up to 24
+// waves the list taken is 2.6 % behind the best on the mean, 9 % at the most.
+// One query: 16 x 64, three texts of about 20,000, 575, 49.8 / 53.3 / 56.0; 512
+// keys, 12 x 64, whole 12.5, shares of 2 / 4 / 8 blocks 6.4 / 7.2 / 9.7; 64 texts
+// of about 96 keys, 16 x 64, whole 8.7, of 2 / 4 blocks 13.0 / 11.7.
 void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv, int n_kv_heads,
                       int group, int d_head, int n_cus, CrossList* out) {
   const Lengths s = {n_seqs, cu_q, cu_kv, group};
