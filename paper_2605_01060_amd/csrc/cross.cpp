@@ -18,8 +18,8 @@ struct Lengths {
   int64_t keys(int64_t i) const { return cu_kv[i + 1] - cu_kv[i]; }
 };
 
-// Units of at most `share` 32-key blocks: a sequence with more is split into
-// equal parts.
+// Units of at most `share` (>= 1) 32-key blocks: a sequence with more is split
+// into equal parts.
 CrossList split_list(const Lengths& s, int64_t share) {
   CrossList out;
   for (int64_t i = 0; i < s.n_seqs; ++i) {
@@ -139,7 +139,10 @@ double list_us(CrossList* list, int n_kv_heads, int d_head, int n_cus) {
 void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv, int n_kv_heads,
                       int group, int d_head, int n_cus, CrossList* out) {
   const Lengths s = {n_seqs, cu_q, cu_kv, group};
-  int64_t work = 0, longest = 0, units = 0;
+  // longest: key blocks of the longest text that is read, a share of them where
+  // none is split.  Texts without queries do not count, so it may be that only
+  // they have states: one block then, as a share of none has no parts.
+  int64_t work = 0, longest = 1, units = 0;
   for (int64_t i = 0; i < n_seqs; ++i) {
     const int64_t rows = s.rows(i), kb = blocks32(s.keys(i));
     work += blocks32(rows) * kb * n_kv_heads;
@@ -160,7 +163,7 @@ void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv,
     out->short_blocks = d_head == 128 && longest > 8;
     return;
   }
-  *out = split_list(s, std::max<int64_t>(longest, 1));
+  *out = split_list(s, longest);
   double best = list_us(out, n_kv_heads, d_head, n_cus);
   int64_t last = longest;
   for (int per_cu : {4, 6, 8}) {

@@ -189,3 +189,37 @@ def test_short_blocks_of_keys_where_the_third_unit_of_a_cu_is_filled(lists):
     assert not short(300, 128, 256, 8, 128)   # of few blocks
     for dh in (32, 64):
         assert not short(96, 128, 1000, 8, dh) and not short(300, 128, 512, 8, dh)
+
+
+@pytest.mark.parametrize("n", [1, 20, 399, 3000])
+@pytest.mark.parametrize("heads,group,dh", [(12, 1, 64), (2, 4, 128)])
+def test_lists_of_queries_without_states_beside_states_without_queries(lists, n, heads, group, dh):
+    """Few units and, from 399 texts on 12 key heads, more than eight a CU: no text
+    that is read has a key, and one that is not read has some."""
+    q, kv = [1] * n + [0], [0] * n + [100]
+    items, joins, n_parts, max_parts, cu = lists(q, kv, heads, group, dh, 256)
+    check_list(q, kv, group, items, joins, n_parts, max_parts, cu)
+    assert n_parts == 0 and len(items[2]) == n
+
+
+@settings(max_examples=100, deadline=None)
+@given(kinds=st.lists(st.tuples(st.sampled_from([0, 0, 1, 33, 130]), st.sampled_from([0, 0, 1, 100, 3000])),
+                      min_size=1, max_size=6),
+       times=st.sampled_from([1, 40, 300]), heads=st.sampled_from([1, 12]),
+       dh=st.sampled_from([64, 128]))
+def test_lists_of_many_texts(lists, kinds, times, heads, dh):
+    """The same, up to 1,800 texts: either length is 0 as often as not."""
+    q, kv = [k[0] for k in kinds] * times, [k[1] for k in kinds] * times
+    items, joins, n_parts, max_parts, cu = lists(q, kv, heads, 2, dh, 64)
+    seen = {}
+    for c, step in enumerate(ROWS):
+        for q_beg, row0, rows, kv_beg, k0, k1, part, _ in items[c].tolist():
+            assert 0 <= row0 < rows and row0 % step == 0 and k1 >= k0
+            seen.setdefault((q_beg, row0), []).append((k0, k1))
+    keys = {int(cu[0][i]): kv[i] for i in range(len(q)) if q[i]}
+    assert {b for b, _ in seen} == set(keys)
+    for (q_beg, _), parts in seen.items():
+        parts.sort()
+        assert parts[0][0] == 0 and parts[-1][1] == keys[q_beg]
+        assert all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
+    assert sum(j[4] for j in joins.tolist()) == n_parts and 2 * len(joins) <= n_parts
