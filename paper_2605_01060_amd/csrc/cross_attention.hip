@@ -50,6 +50,7 @@
 // run under the exponentials of this one (48 spilled registers at d_head 128,
 // 410 -> 523 us); the sum of the rounded probabilities by dot products (-1 to
 // -2 %); four waves per SIMD at d_head 32 (16 spilled, 189 -> 242 us).
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -174,6 +175,7 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
     return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
+  bool seen = false;  // any key so far: one for all rows
   float m_ref = -INFINITY, l_run = 0.0f;
   f32x16 o[DT];
 #pragma unroll
@@ -192,6 +194,7 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const bool on = byte != 0 && i * KB + (lane & (KB - 1)) < n_keys;
     const uint64_t keys = __ballot(on) & FULL;
+    seen = seen || keys;
     if (keys != FULL) {
       // Absent keys: -inf in the accumulators that their scores start from, and
       // zeros over what stands in their rows of K and V, where a NaN or an
@@ -311,7 +314,9 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
   }
   if (row0 + col >= item.rows) return;
   const int64_t slot = ((int64_t)(item.part + wave) * a.n_kv_heads + kvh) * 32 + col;
-  if (half == 0) a.part_ml[slot] = make_float2(m_ref, l_run);
+  // -inf is the maximum of a part without keys alone: one of NaN scores, which
+  // leave the maximum where it was, has a NaN sum and output to be joined.
+  if (half == 0) a.part_ml[slot] = make_float2(seen ? fmaxf(m_ref, -FLT_MAX) : -INFINITY, l_run);
   float* po = a.part_o + slot * DH;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void cross_join_kernel(CrossAtte
   float l = 0.0f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-  // Without any key in the row (m = -inf) every part is zeros: nothing to add.
+  // Without any key for the row (m = -inf) every part is zeros: nothing to add.
   for (int p0 = wave; p0 < j.parts && m > -INFINITY; p0 += WAVES * BATCH) {
     float2 ml[BATCH];
     float v[BATCH][PER];

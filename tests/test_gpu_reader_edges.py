@@ -6,7 +6,7 @@ import pytest
 
 from gpu_util import torch_cuda
 from paper_2605_01060_amd import surge as S
-from test_gpu_reader import cross_call, cross_inputs
+from test_gpu_reader import cross_call, cross_inputs, cross_reference, within
 
 pytestmark = pytest.mark.gpu
 
@@ -17,3 +17,58 @@ def test_cross_attention_of_many_queries_without_states_beside_states_without_qu
     out = torch.full((400, 12 * 64), 7.0, dtype=torch.bfloat16, device="cuda")
     cross_call(p, out)
     assert (out[:399] == 0).all() and (out[399] == 7).all()
+
+
+def agrees(got, ref, tol):
+    """NaN where the reference has it and nowhere else, and the rest within tol."""
+    torch = torch_cuda()
+    bad = ref.isnan()
+    assert torch.equal(got.isnan(), bad), (int(got.isnan().sum()), int(bad.sum()))
+    if not bad.all():
+        within(got[~bad], ref[~bad], tol[~bad])
+
+
+# Sequences of one unit or more per key head, of every height, whole and with
+# their keys split: queries, states, heads, key heads, d_head, split.
+SHAPES = [([1], [50], 4, 2, 64, False), ([3, 1], [130, 40], 2, 2, 32, False), ([9], [77], 8, 2, 128, False),
+          ([50], [300], 2, 2, 64, True), ([33], [90], 2, 1, 128, False), ([70], [300], 4, 4, 32, False),
+          ([40] * 6, [90, 60, 70, 100, 33, 50], 2, 2, 64, False), ([40] * 60, [100] * 60, 8, 8, 64, False),
+          ([200, 1], [200, 9], 2, 2, 128, False), ([1], [9000], 4, 2, 64, True), ([1], [20_011], 32, 8, 128, True),
+          ([3], [8193], 2, 2, 32, True), ([40], [3001], 2, 2, 64, True), ([200], [2049], 2, 2, 128, True),
+          ([150], [4097], 8, 2, 64, True), ([1], [70_001], 1, 1, 128, True)]
+
+
+def cross_out(p, split):
+    torch = torch_cuda()
+    out = torch.full((p["q"].shape[0], p["heads"] * p["dh"]), 7.0, dtype=torch.bfloat16, device="cuda")
+    plan, _ = cross_call(p, out)
+    assert (plan.n_parts > 0) == split
+    return out
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+@pytest.mark.parametrize("mask", [None, 0.3])
+def test_cross_attention_of_a_nan_query(q, kv, heads, kv_heads, dh, split, mask):
+    """NaN in one head of a query: that head's output, and no other, is NaN."""
+    torch = torch_cuda()
+    p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv), mask)
+    t, h = sum(q) // 2, heads - 1
+    p["q"][t, h * dh + 5] = math.nan
+    ref, tol = cross_reference(p)
+    assert int(ref.isnan().sum()) == dh
+    agrees(cross_out(p, split), ref, tol)
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+def test_cross_attention_of_nan_states(q, kv, heads, kv_heads, dh, split):
+    """NaN in a state's key: all rows that read it; in all keys: all rows; in a
+    state's value: that feature."""
+    torch = torch_cuda()
+    p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv))
+    clean, w = p["kv"].clone(), kv_heads * dh
+    for rows, col in ((kv[0] - 1, 3), (slice(0, kv[0]), 3), (kv[0] // 2, w + dh - 1)):
+        p["kv"].copy_(clean)
+        p["kv"][rows, col] = math.nan
+        ref, tol = cross_reference(p)
+        assert ref.isnan().any() and (len(q) == kv_heads == 1 or not ref.isnan().all())
+        agrees(cross_out(p, split), ref, tol)
