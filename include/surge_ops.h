@@ -233,7 +233,9 @@ surge_status surge_cross_plan_info(const surge_cross_plan* plan, int64_t* worksp
 /*
  * Cross attention: out[t][h] = sum_k p_k v[k] / sum_k p_k over the states k
  * of t's text, p_k = exp(scale q[t][h] . k[k]); a sequence without states, or
- * with none left by the mask, gives zeros.
+ * with none left by the mask, gives zeros.  Scores, log2(e) scale q . k, are
+ * fp32: a row of which one is a NaN, the largest overflows or none is above
+ * -infinity gives NaN.
  * d_q, d_out bf16 [cu_q[n], n_heads d_head]; d_k, d_v bf16 [cu_kv[n],
  * n_kv_heads d_head] (two column ranges of one projection's output, say, with
  * its stride); d_key_mask one byte per state, 0 leaves it out (what stands in

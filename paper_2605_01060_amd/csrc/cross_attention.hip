@@ -289,7 +289,8 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
     // registers are four times as many requests).
     __syncthreads();  // every wave has read its last block
     if (!active) return;
-    const float inv = l_run > 0.0f ? 1.0f / l_run : 0.0f;
+    // A sum of 0 over some keys (scores that overflow) is no row without keys.
+    const float inv = seen ? 1.0f / l_run : 0.0f;
     u32x4* stage = sKV + wave * (32 * CPR);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void cross_join_kernel(CrossAtte
         if (lane < DH) o[i] += so[w][lane * PER + i];
     }
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = m > -INFINITY ? 1.0f / l : 0.0f;
   const int row = j.row0 + r;
   uint16_t* out = a.out + ((int64_t)j.q_beg + row / a.group) * a.ld_out + (kvh * a.group + row % a.group) * DH;
   if constexpr (PER == 2)

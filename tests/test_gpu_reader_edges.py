@@ -72,3 +72,19 @@ def test_cross_attention_of_nan_states(q, kv, heads, kv_heads, dh, split):
         ref, tol = cross_reference(p)
         assert ref.isnan().any() and (len(q) == kv_heads == 1 or not ref.isnan().all())
         agrees(cross_out(p, split), ref, tol)
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_cross_attention_of_scores_past_the_largest_float(q, kv, heads, kv_heads, dh, split, sign):
+    """scale q . k overflows at every state of the first text: NaN, not the
+    zeros of a text without states."""
+    torch = torch_cuda()
+    p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv))
+    p["scale"] = 1e38
+    p["q"][:] = 1.0
+    p["kv"][:kv[0], :kv_heads * dh] = sign
+    p["kv"][kv[0]:, :kv_heads * dh] = 0
+    out = cross_out(p, split)
+    assert out[:q[0]].isnan().all()
+    assert torch.isfinite(out[q[0]:]).all()
