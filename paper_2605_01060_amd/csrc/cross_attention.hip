@@ -175,8 +175,10 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
     return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
   };
 
+  // The maximum starts from the lowest finite value, which scores of -inf don't
+  // move: their exponentials are 0 against it, and NaN against themselves.
   bool seen = false;  // any key so far: one for all rows
-  float m_ref = -INFINITY, l_run = 0.0f;
+  float m_ref = -FLT_MAX, l_run = 0.0f;
   f32x16 o[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
@@ -317,7 +319,7 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
   const int64_t slot = ((int64_t)(item.part + wave) * a.n_kv_heads + kvh) * 32 + col;
   // -inf is the maximum of a part without keys alone: one of NaN scores, which
   // leave the maximum where it was, has a NaN sum and output to be joined.
-  if (half == 0) a.part_ml[slot] = make_float2(seen ? fmaxf(m_ref, -FLT_MAX) : -INFINITY, l_run);
+  if (half == 0) a.part_ml[slot] = make_float2(seen ? m_ref : -INFINITY, l_run);
   float* po = a.part_o + slot * DH;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)

@@ -88,3 +88,41 @@ def test_cross_attention_of_scores_past_the_largest_float(q, kv, heads, kv_heads
     out = cross_out(p, split)
     assert out[:q[0]].isnan().all()
     assert torch.isfinite(out[q[0]:]).all()
+
+
+def lowest_keys(p, rows):
+    """Scores of -inf at these states, for every row: 1 times -inf in one feature."""
+    torch = torch_cuda()
+    dh = p["dh"]
+    p["q"][:, 0::dh] = 1.0
+    p["kv"][rows, 0:p["kv_heads"] * dh:dh] = -math.inf
+    seen = torch.ones(p["kv"].shape[0], dtype=torch.uint8, device="cuda")
+    seen[rows] = 0
+    return {**p, "mask": seen if p["mask"] is None else p["mask"] * seen}
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+@pytest.mark.parametrize("mask", [None, 0.3])
+def test_cross_attention_of_scores_of_minus_infinity(q, kv, heads, kv_heads, dh, split, mask):
+    """A text's first half (whole blocks and parts) scores -inf: its
+    probabilities are 0, as if it were masked."""
+    torch = torch_cuda()
+    p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv), mask)
+    ref, tol = cross_reference(lowest_keys(p, slice(0, (kv[0] + 1) // 2)))
+    agrees(cross_out(p, split), ref, tol)
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+def test_cross_attention_of_rows_without_a_finite_score(q, kv, heads, kv_heads, dh, split):
+    """All of a text's scores are -inf, or its masked rest is all that is not:
+    0 / 0, which is not the zeros of a text without states."""
+    torch = torch_cuda()
+    for mask in (None, 0.3):
+        p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv), mask)
+        lowest_keys(p, slice(0, kv[0]))
+        if mask is not None:
+            p["mask"][:kv[0]] = 0
+            p["mask"][kv[0] // 3] = 1
+        out = cross_out(p, split)
+        assert out[:q[0]].isnan().all()
+        assert torch.isfinite(out[q[0]:]).all()
