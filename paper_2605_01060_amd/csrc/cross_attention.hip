@@ -196,7 +196,6 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     const bool on = byte != 0 && i * KB + (lane & (KB - 1)) < n_keys;
     const uint64_t keys = __ballot(on) & FULL;
-    seen = seen || keys;
     if (keys != FULL) {
       // Absent keys: -inf in the accumulators that their scores start from, and
       // zeros over what stands in their rows of K and V, where a NaN or an
@@ -217,6 +216,7 @@ __attribute__((amdgpu_waves_per_eu(DH == 128 && KB == 64 ? 2 : 3))) void cross_k
       byte = mask_byte(i + 1);
     }
     if (active && keys) {
+      seen = true;
       f32x16 s[T];
       // Ahead of the waves of the SIMD that are at their exponentials.
       __builtin_amdgcn_s_setprio(1);
