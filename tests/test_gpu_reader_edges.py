@@ -6,7 +6,7 @@ import pytest
 
 from gpu_util import torch_cuda
 from paper_2605_01060_amd import surge as S
-from test_gpu_reader import cross_call, cross_inputs, cross_reference, within
+from test_gpu_reader import BF16, F32, cross_call, cross_inputs, cross_reference, gen, within
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +126,28 @@ def test_cross_attention_of_rows_without_a_finite_score(q, kv, heads, kv_heads, 
         out = cross_out(p, split)
         assert out[:q[0]].isnan().all()
         assert torch.isfinite(out[q[0]:]).all()
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_cross_attention_of_scores_whose_float_steps_are_large(q, kv, heads, kv_heads, dh, split, sign):
+    """Scores of 2^20 to 2^100 and their multiples by 1 to 50: the states of the
+    largest share a row, in equal parts, whatever a step of a float is there."""
+    torch = torch_cuda()
+    p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv))
+    w, tk = kv_heads * dh, sum(kv)
+    level = sign * (torch.randperm(tk, generator=gen(sum(kv)), device="cuda") % 50 + 1)
+    p["q"].zero_()
+    p["kv"][:, :w] = 0
+    p["kv"][:, 0:w:dh] = level[:, None].bfloat16()
+    want = []
+    for i, n in enumerate(q):
+        at = slice(int(p["cu_kv"][i]), int(p["cu_kv"][i + 1]))
+        top = p["kv"][at, w:][level[at] == level[at].max()].double().view(-1, kv_heads, dh)
+        want.append(torch.stack([top.mean(0), top.abs().mean(0)])[:, None].repeat_interleave(heads // kv_heads, 2)
+                    .expand(2, n, heads, dh).reshape(2, n, heads * dh))
+    ref, size = torch.cat(want, 1)
+    for e in (20, 28, 33, 40, 100):
+        p["q"][:, 0::dh] = 2.0 ** e
+        # Equal probabilities, up to a rounding to bf16, and the sums.
+        within(cross_out(p, split), ref, BF16 * ref.abs() + (1.01 * BF16 + tk * F32) * size, e)
