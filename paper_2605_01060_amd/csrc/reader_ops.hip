@@ -28,7 +28,8 @@ struct surge_cross_plan {
   int n_kv_heads = 0, group = 0, d_head = 0;
   int64_t q_tokens = 0, kv_tokens = 0;
   int n_items[CROSS_CLASSES] = {}, n_units = 0, n_joins = 0, max_parts = 0;
-  int64_t n_parts = 0;
+  int64_t n_parts = 0;   // slots of 32 rows in the workspace
+  int n_split = 0;       // of the units, those that hold a part of their rows' keys
   bool short_blocks = false;
   void* lists = nullptr;  // device: the items of each class, then the joins
 };
@@ -282,6 +283,8 @@ surge_status surge_cross_plan_create(int64_t n_seqs, const int64_t* h_cu_q, cons
     p->kv_tokens = h_cu_kv[n_seqs];
     for (int c = 0; c < CROSS_CLASSES; ++c) p->n_items[c] = (int)list.items[c].size();
     p->n_units = (int)items;
+    for (const auto& v : list.items)
+      for (const CrossItem& it : v) p->n_split += it.part >= 0;
     p->n_joins = (int)list.joins.size();
     p->max_parts = list.max_parts;
     p->n_parts = list.n_parts;
@@ -329,7 +332,7 @@ surge_status surge_cross_plan_info(const surge_cross_plan* plan, int64_t* bytes,
   if (!plan) return fail(SURGE_ERR_INVALID_ARGUMENT, "plan is NULL");
   if (bytes) *bytes = workspace_bytes(plan);
   if (n_units) *n_units = (int64_t)plan->n_units * plan->n_kv_heads;
-  if (n_parts) *n_parts = plan->n_parts * plan->n_kv_heads;
+  if (n_parts) *n_parts = (int64_t)plan->n_split * plan->n_kv_heads;
   return SURGE_OK;
 }
 

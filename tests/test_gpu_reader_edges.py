@@ -6,7 +6,8 @@ import pytest
 
 from gpu_util import torch_cuda
 from paper_2605_01060_amd import surge as S
-from test_gpu_reader import BF16, F32, cross_call, cross_inputs, cross_reference, gen, within
+from test_gpu_reader import (BF16, F32, cross_call, cross_inputs, cross_reference,
+                             cu_of, gen, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -151,3 +152,14 @@ def test_cross_attention_of_scores_whose_float_steps_are_large(q, kv, heads, kv_
         p["q"][:, 0::dh] = 2.0 ** e
         # Equal probabilities, up to a rounding to bf16, and the sums.
         within(cross_out(p, split), ref, BF16 * ref.abs() + (1.01 * BF16 + tk * F32) * size, e)
+
+
+def test_cross_plan_counts_the_units_that_hold_a_part():
+    """Units of 128 and of 64 rows, all split, beside whole ones of a short text."""
+    for q, rows in ((200, 128), (50, 64), (1, 32)):
+        alone = S.CrossPlan(cu_of([q]), cu_of([40_000]), 2, 2, 64)
+        assert alone.n_units == alone.n_parts > 2 * -(-q // rows)
+        both = S.CrossPlan(cu_of([q, 130]), cu_of([40_000, 7]), 2, 2, 64)
+        assert both.n_units - both.n_parts == 2 * 2
+        whole = S.CrossPlan(cu_of([q]), cu_of([20]), 2, 2, 64)
+        assert whole.n_parts == 0 and whole.n_units == 2 * -(-q // rows)
