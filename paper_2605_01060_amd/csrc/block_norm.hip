@@ -186,7 +186,8 @@ struct Affine {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           g[j][i] *= f[i];
-          b[j][i] *= f[i];
+          // No beta stays 0 under an infinite gate.
+          if (beta) b[j][i] *= f[i];
         }
       }
     }

@@ -6,8 +6,8 @@ import pytest
 
 from gpu_util import torch_cuda
 from paper_2605_01060_amd import surge as S
-from test_gpu_reader import (BF16, F32, cross_call, cross_inputs, cross_reference,
-                             cu_of, gen, within)
+from test_gpu_reader import (BF16, F32, block_norm, cross_call, cross_inputs,
+                             cross_reference, cu_of, gen, norm_inputs, norm_reference, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -163,3 +163,21 @@ def test_cross_plan_counts_the_units_that_hold_a_part():
         assert both.n_units - both.n_parts == 2 * 2
         whole = S.CrossPlan(cu_of([q]), cu_of([20]), 2, 2, 64)
         assert whole.n_parts == 0 and whole.n_units == 2 * -(-q // rows)
+
+
+@pytest.mark.parametrize("kind", [S.NORM_LAYER, S.NORM_RMS])
+@pytest.mark.parametrize("d", [40, 768, 2056, 8192])
+@pytest.mark.parametrize("post", [False, True])
+def test_block_norm_of_an_infinite_gate(kind, d, post):
+    """An infinity of the gate's sign and the block's, without a beta that it
+    could meet as 0 times infinity."""
+    torch = torch_cuda()
+    M = 7
+    p = norm_inputs(M, d, False, post, "vector", True, d + kind)
+    p["gate"][d // 3], p["gate"][d - 1] = math.inf, -math.inf
+    y = torch.empty(M, d, dtype=torch.bfloat16, device="cuda")
+    block_norm(p, M, d, kind, 0.7, y)
+    ry, ey, _, _ = norm_reference(p, kind == S.NORM_LAYER, 0.7, d)
+    inf = ry.isinf()
+    assert inf.sum() == 2 * M and torch.equal(y.double()[inf], ry[inf])
+    within(y[~inf], ry[~inf], (BF16 * ry.abs() + 1.01 * ey)[~inf])
