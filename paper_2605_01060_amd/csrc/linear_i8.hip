@@ -621,13 +621,6 @@ void launch_ring(int64_t M, int N, int K, const LinearI8& a, hipStream_t stream)
                      dim3(64 * WAVES_M * WAVES_N), 0, stream, a, (int)M, N, K, tiles_n, n_tiles);
 }
 
-template <int J, int EPI>
-void launch_tokens(int64_t M, int N, int K, const LinearI8& a, hipStream_t stream) {
-  hipLaunchKernelGGL((linear_i8_tokens_kernel<J, EPI>),
-                     dim3((N + 15) / 16, (unsigned)((M + 16 * J - 1) / (16 * J))), dim3(512), 0, stream, a,
-                     (int)M, N, K);
-}
-
 template <int WAVES_M, int WAVES_N, int TI, int J0, int EPI>
 void launch_wide(int64_t M, int N, int K, const LinearI8& a, int n_cus, hipStream_t stream) {
   constexpr int BM = WAVES_M * 16 * (J0 + 2);
