@@ -181,3 +181,65 @@ def test_block_norm_of_an_infinite_gate(kind, d, post):
     inf = ry.isinf()
     assert inf.sum() == 2 * M and torch.equal(y.double()[inf], ry[inf])
     within(y[~inf], ry[~inf], (BF16 * ry.abs() + 1.01 * ey)[~inf])
+
+
+def underflowed(p):
+    """What the keys add whose probability is below 2^-118 of their row's
+    largest.  The reference of the exponentials is at most 2^8 below the largest
+    score, so the others stay above the least normal float 2^-126 wherever they
+    are formed (of a unit's keys, or as a part's weight times one of at most
+    2^8); these may be flushed to 0, and lose what they add at the most."""
+    torch = torch_cuda()
+    heads, kv_heads, dh = p["heads"], p["kv_heads"], p["dh"]
+    group, w = heads // kv_heads, kv_heads * dh
+    lost = torch.zeros(p["q"].shape, dtype=torch.float64, device="cuda")
+    for i in range(len(p["cu_q"]) - 1):
+        r, c = (slice(int(cu[i]), int(cu[i + 1])) for cu in (p["cu_q"], p["cu_kv"]))
+        k = p["kv"][c, :w].double().view(-1, kv_heads, dh).permute(1, 2, 0).contiguous()
+        v = p["kv"][c, w:].double().view(-1, kv_heads, dh).permute(1, 0, 2).contiguous()
+        q = p["q"][r].double().view(-1, kv_heads, group, dh).permute(1, 0, 2, 3).reshape(kv_heads, -1, dh)
+        prob = torch.softmax(torch.bmm(q, k) * p["scale"], 2)
+        prob = torch.where(prob < 2.0 ** -118 * prob.amax(2, keepdim=True), prob, 0.0)
+        lost[r] = torch.bmm(prob, v.abs()).view(kv_heads, -1, group, dh).permute(1, 0, 2, 3) \
+            .reshape(-1, heads * dh)
+    return lost
+
+
+@pytest.mark.parametrize("q,kv,heads,kv_heads,dh,split", SHAPES)
+@pytest.mark.parametrize("nats", [5.0, 7.0, 12.0])
+@pytest.mark.parametrize("rows", ["rise", "fall", "both"])
+def test_cross_attention_of_scores_that_rise_from_block_to_block(q, kv, heads, kv_heads, dh, split, nats, rows):
+    """Eight stretches of a text whose scores differ by `nats` from one to the
+    next, up or down or, in rows beside each other, both, and values that make
+    up for it: every stretch counts in the output (of rows of one sign), so
+    each rescaling of the sums is seen.  Scores of up to 100: the tolerance has
+    them in it."""
+    torch = torch_cuda()
+    p = cross_inputs(q, kv, heads, kv_heads, dh, sum(kv) + int(nats))
+    w = kv_heads * dh
+    up = torch.ones(sum(q), device="cuda")
+    if rows == "fall":
+        up = -up
+    if rows == "both":
+        up[1::2] = -1
+    for i, (a, n) in enumerate(zip(p["cu_kv"], kv)):
+        level = torch.arange(n, device="cuda") * 8 // n - 3.5
+        p["kv"][a:a + n, 0:w:dh] = (level * nats * math.sqrt(dh) / 8)[:, None].bfloat16()
+        sign = -1.0 if rows == "fall" else 1.0
+        p["kv"][a:a + n, w:] *= torch.exp(-sign * level * nats)[:, None]
+    p["q"][:, 0::dh] = (8 * up)[:, None].bfloat16()
+    ref, tol = cross_reference(p)
+    within(cross_out(p, split), ref, tol + underflowed(p))
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_cross_attention_of_large_scores(dh):
+    """Scores of hundreds and thousands against the definition."""
+    torch = torch_cuda()
+    p = cross_inputs([40, 1, 200, 2], [300, 4000, 500, 0], 2, 2, dh, 3)
+    p["q"] *= 100
+    p["kv"][:, :2 * dh] *= 10
+    ref, tol = cross_reference(p)
+    out = torch.empty_like(p["q"])
+    cross_call(p, out)
+    within(out, ref, tol)
