@@ -190,7 +190,8 @@ int32_t surge_op_linear_i8_tile(int64_t M, int32_t N, int32_t K, int32_t n_cus);
  * bf16 [M, d], the next block's input; d_zq int8 with d_zq_scale fp32 [M],
  * the same rows as surge_op_quantize_rows gives them, before a rounding to
  * bf16 (d_zq has d rounded up to a multiple of 128 columns).  Each output may
- * be NULL, not all.  z is made from y before its rounding to bf16.
+ * be NULL, not all.  z is made from y before its rounding to bf16.  Sums over
+ * a row are fp32: where that of the squares overflows, the norm is of zeros.
  * NULL inputs: d_block (y = res_scale * x; then no post norm or gate),
  * d_post_gamma (no norm after the block), either beta (0; always NULL for
  * SURGE_NORM_RMS), d_gate, d_gate_rows (1).  d_pre_gamma is needed for z.
@@ -235,7 +236,10 @@ surge_status surge_cross_plan_info(const surge_cross_plan* plan, int64_t* worksp
  * of t's text, p_k = exp(scale q[t][h] . k[k]); a sequence without states, or
  * with none left by the mask, gives zeros.  Scores, log2(e) scale q . k, are
  * fp32: a row of which one is a NaN, the largest overflows or none is above
- * -infinity gives NaN.
+ * -infinity gives NaN.  Maxima, sums and outputs are fp32; each p_k is rounded
+ * to bf16, the type of v, for its product with v, but not in the sum of p_k:
+ * outputs are off by up to 2^-8 of sum_k p_k |v[k]| / sum_k p_k, and their own
+ * rounding.
  * d_q, d_out bf16 [cu_q[n], n_heads d_head]; d_k, d_v bf16 [cu_kv[n],
  * n_kv_heads d_head] (two column ranges of one projection's output, say, with
  * its stride); d_key_mask one byte per state, 0 leaves it out (what stands in

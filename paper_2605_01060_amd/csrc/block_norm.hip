@@ -9,10 +9,11 @@
 // E[v^2] - mean^2 cancellation), and all sums are fp32.
 //
 // What bounds them, measured: memory.  200,003 rows of 1024 with gate rows take
-// 341 us (6.0 TB/s for 2.05 GB), quantizing 200,003 rows of 4096 366 us (6.7
-// TB/s), where a large copy reaches 4.9.  Rows of a few thousand: 13,579 of 768
-// 20.3 us (4.1 TB/s), a wave's five rows one after the other.  Small calls: 64
-// rows of 1024 4 us, the chain of a row's loads and its four reductions.
+// 340 to 350 us (5.8 to 6.0 TB/s for 2.05 GB), quantizing 200,003 rows of 4096
+// 366 to 400 us (6.1 to 6.7 TB/s), where a large copy reaches 4.8.  Rows of a few
+// thousand: 13,579 of 768 to int8 21 to 22 us (3.4 TB/s), a wave's five rows one
+// after the other at three waves per SIMD (148 registers).  Small calls: 64 rows
+// of 1024 4 us, the chain of a row's loads and its four reductions.
 #include <math.h>
 
 #include <algorithm>
@@ -195,6 +196,7 @@ struct Affine {
 };
 
 // v <- (v - mean) / sqrt(var + eps) over the row, or v / sqrt(mean v^2 + eps).
+// The sum of squares is fp32: where it overflows, 1 / sqrt is 0.
 // Chunks past the row hold 0 and stay out of the variance.
 template <int LANES, int CH, bool RMS>
 __device__ __forceinline__ void normalise(float (&v)[CH][8], int lane, int chunks, float inv_d, float eps,

@@ -128,14 +128,23 @@ double list_us(CrossList* list, int n_kv_heads, int d_head, int n_cus) {
 // of its rows.  Few large units leave CUs idle at the end or wait for one
 // wave's chain of blocks, many cost the join, and which is less depends on the
 // lengths: the list with the least time by list_us is taken.  Measured (us,
-// whole, then shares of 4 / 6 / 8 waves per CU): heads 16 / 4 x 128, four texts
-// of about 6000, 1500 queries each, 300, 300 / 322 / 290; 16 x 64, 7 texts of
-// about 5000, 300 queries, 160, 129 / 113 / 119; 12 x 64, two of about 9000,
-// 2000 queries, 134, 119 / 91 / 100; over 12 such calls and shares of up to 24
-// waves the list taken is 2.6 % behind the best on the mean, 9 % at the most.
-// One query: 16 x 64, three texts of about 20,000, 575, 49.8 / 53.3 / 56.0; 512
-// keys, 12 x 64, whole 12.5, shares of 2 / 4 / 8 blocks 6.4 / 7.2 / 9.7; 64 texts
-// of about 96 keys, 16 x 64, whole 8.7, of 2 / 4 blocks 13.0 / 11.7.
+// whole, then shares of 4 / 6 / 8 waves per CU, * the list taken):
+//   texts x queries x keys, heads
+//   4 x 1500 x about 6000, 16 / 4 x 128   317, 316 / 314 / 284*
+//   3 x 1500 x 15,000, 8 / 1 x 128        379, 381 / 330 / 330*
+//   6 x 500 x 10,000, 16 / 4 x 128        275*, 275 / 260 / 260
+//   7 x 300 x 5000, 16 x 64               98, 98 / 83 / 83*
+//   2 x 2000 x 9000, 12 x 64              174, 175 / 153 / 153*
+//   10 x 300 x 2000, 8 x 128              43.7*, 49.4 / 49.4 / 49.2
+//   1 x 1000 x 1000, 16 / 4 x 128         24.0, 25.9* / 28.5 / 28.3
+//   1 x 256 x 50,000, 8 x 128             946, 88 / 88 / 81*
+//   2 x 100 x 30,000, 12 x 32             333, 52 / 43 / 41*
+//   3 x 40 x 20,000, 16 x 64              385, 63* / 50 / 48
+//   3 x 1 x about 20,000, 16 x 64         517, 38* / 41 / 42
+//   64 x 1 x about 96, 16 x 64            7.2*, 9.0 / 9.2 / 10.0
+//   1 x 1 x 512, 12 x 64                  12.7, 6.9* / 6.8 / 6.8
+// The list taken is 3 % behind the best of these on the mean, 28 % in the call of
+// 40 queries.
 void build_cross_list(int64_t n_seqs, const int64_t* cu_q, const int64_t* cu_kv, int n_kv_heads,
                       int group, int d_head, int n_cus, CrossList* out) {
   const Lengths s = {n_seqs, cu_q, cu_kv, group};

@@ -34,17 +34,17 @@
 // fill the third place (measured, 64 / 32 keys, us: 6 sequences, 500 queries,
 // about 10,000 keys, 16 / 4 heads 450 / 398; 4, 1500, 6000 with a mask
 // 328 / 309) and 64 where they don't (10 sequences, 300, about 2000, 8 heads
-// 48 / 53; 1, 1000, 1000, 16 / 4 24 / 28) or have few blocks (1000, 128, 128, 8
-// heads 192 / 197).
+// 48 / 53) or have few blocks (1000, 128, 128, 8 heads 192 / 197).
 //
 // What bounds it, measured: many rows, the power limit and the exponentials.
-// 8 sequences, 2048 queries, 8192 keys, 16 heads x 128 take 1,010 to 1,060 us,
-// 1,040 to 1,090 TFLOP/s, at 1.8 GHz with the MFMA pipe half busy; 16 x 64 (4096
-// queries) 951 TFLOP/s, 16 x 32 687, where a score costs the VALU the same and
-// the MFMAs a half and a quarter.  Few rows, memory: one query of 32 / 8 heads x 128 over
-// 100,003 keys streams them in 74 us, 5.5 TB/s, and joins in 6.  Small calls, a
-// wave's chain: about 0.6 us per block of 32 keys (MFMA and LDS latencies; a
-// deeper ring of blocks changes nothing).
+// 8 sequences, 2048 queries, 8192 keys, 16 heads x 128 take 1,060 to 1,080 us,
+// 1,020 to 1,040 TFLOP/s, at 1.7 to 1.8 GHz with the MFMA pipe and the VALU half
+// busy; 16 x 64 take 615 to 620 us, 890 TFLOP/s, 16 x 32 429, 640, where a score
+// costs the VALU the same (78 and 92 % busy) and the MFMAs a half and a quarter.
+// Few rows, memory: one query of 32 / 8 heads x 128 over 100,003 keys streams them
+// in 74 to 78 us, 5.3 to 5.5 TB/s, and joins in 6.  Small calls, a wave's chain:
+// about 0.6 us per block of 32 keys (MFMA and LDS latencies; a deeper ring of
+// blocks changes nothing).
 //
 // Tried and dropped: K a block ahead of V, so that the scores of the next block
 // run under the exponentials of this one (48 spilled registers at d_head 128,

@@ -9,16 +9,18 @@
 // chunks, read from LDS rows whose chunk c of row r sits at c ^ (r & 7).
 //
 // Three kinds of kernel, chosen by a model of their times (below): persistent
-// 256 x 256 and 192 x 256 tiles with the schedule of linear_wide.hip, rings of
+// 256 x 256 and 192 x 256 tiles with the schedule of linear_wide.hip (its waits
+// and barriers stand there a second time: a mend of one is one of both), rings of
 // one tile per workgroup for launches of few tiles, and a kernel for few
 // tokens.
 //
-// What bounds them, measured: large K, the power limit (8192^3 in 380 us, 2,892
-// TOP/s; M = 200,003, N = 1024, K = 4096 with residual 735 us, 2,280); K = 768, the
-// epilogue, during which a CU's MFMA pipe idles (M = 200,003, N = 2304: 393 us,
-// 1,800 TOP/s at 2.0 GHz, MFMA pipe 45 % busy, VALU 26 %); few tiles, a tile's
-// chain of K stages (0.26 us each); one token, 2.7 us, the latencies of a launch,
-// two loads and a meeting of eight waves.
+// What bounds them, measured: large K, the power limit (8192^3 in 380 us where
+// the card is cool, 2,892 TOP/s, in 449 many times in a row, 2,450; M = 200,003, N =
+// 1024, K = 4096 with residual 730 to 820 us, 2,050 to 2,300); K = 768, the
+// epilogue, during which a CU's MFMA pipe idles (M = 200,003, N = 2304: 370 to 430
+// us, 1,650 to 1,910 TOP/s at 1.9 GHz, MFMA pipe 49 % busy, VALU 41 %); few tiles, a
+// tile's chain of K stages (0.26 us each); one token, 2.9 us, the latencies of a
+// launch, two loads and a meeting of eight waves.
 //
 // Tried and dropped: starting the CUs apart, so that their stores do not come
 // at once (it costs its delay and gains nothing); the channel vectors in
