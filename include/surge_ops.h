@@ -190,11 +190,12 @@ int32_t surge_op_linear_i8_tile(int64_t M, int32_t N, int32_t K, int32_t n_cus);
  * bf16 [M, d], the next block's input; d_zq int8 with d_zq_scale fp32 [M],
  * the same rows as surge_op_quantize_rows gives them, before a rounding to
  * bf16 (d_zq has d rounded up to a multiple of 128 columns).  Each output may
- * be NULL, not all.  z is made from y before its rounding to bf16.  Sums over
- * a row are fp32: where that of the squares overflows, the norm is of zeros.
+ * be NULL, not all.  z is made from y before its rounding to bf16.
  * NULL inputs: d_block (y = res_scale * x; then no post norm or gate),
  * d_post_gamma (no norm after the block), either beta (0; always NULL for
  * SURGE_NORM_RMS), d_gate, d_gate_rows (1).  d_pre_gamma is needed for z.
+ * d_gate is multiplied into d_post_gamma and d_post_beta first: it is finite
+ * wherever that beta is not 0.
  * d % 8 == 0, d <= 8192; eps in [0, 1].  d_y and d_z may each be d_x, d_block
  * or d_gate_rows with the same stride (not the same one); otherwise outputs
  * must not overlap inputs or each other.

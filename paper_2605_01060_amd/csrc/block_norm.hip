@@ -187,8 +187,8 @@ struct Affine {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           g[j][i] *= f[i];
-          // No beta stays 0 under an infinite gate.
-          if (beta) b[j][i] *= f[i];
+          // A beta of 0, or none, stays 0 under an infinite gate.
+          b[j][i] = b[j][i] == 0.0f ? 0.0f : b[j][i] * f[i];
         }
       }
     }

@@ -243,3 +243,18 @@ def test_cross_attention_of_large_scores(dh):
     out = torch.empty_like(p["q"])
     cross_call(p, out)
     within(out, ref, tol)
+
+
+@pytest.mark.parametrize("d", [40, 768, 2056, 8192])
+def test_block_norm_of_an_infinite_gate_over_a_beta_of_0(d):
+    torch = torch_cuda()
+    M = 7
+    p = norm_inputs(M, d, True, True, "vector", True, d)
+    for i, gate in ((d // 3, math.inf), (d - 1, -math.inf)):
+        p["gate"][i], p["post_beta"][i] = gate, 0.0
+    y = torch.empty(M, d, dtype=torch.bfloat16, device="cuda")
+    block_norm(p, M, d, S.NORM_LAYER, 0.7, y)
+    ry, ey, _, _ = norm_reference(p, True, 0.7, d)
+    inf = ry.isinf()
+    assert inf.sum() == 2 * M and torch.equal(y.double()[inf], ry[inf])
+    within(y[~inf], ry[~inf], (BF16 * ry.abs() + 1.01 * ey)[~inf])
