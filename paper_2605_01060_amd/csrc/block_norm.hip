@@ -14,6 +14,7 @@
 // thousand: 13,579 of 768 to int8 21 to 22 us (3.4 TB/s), a wave's five rows one
 // after the other at three waves per SIMD (148 registers).  Small calls: 64 rows
 // of 1024 4 us, the chain of a row's loads and its four reductions.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -196,7 +197,6 @@ struct Affine {
 };
 
 // v <- (v - mean) / sqrt(var + eps) over the row, or v / sqrt(mean v^2 + eps).
-// The sum of squares is fp32: where it overflows, 1 / sqrt is 0.
 // Chunks past the row hold 0 and stay out of the variance.
 template <int LANES, int CH, bool RMS>
 __device__ __forceinline__ void normalise(float (&v)[CH][8], int lane, int chunks, float inv_d, float eps,
@@ -217,7 +217,23 @@ __device__ __forceinline__ void normalise(float (&v)[CH][8], int lane, int chunk
       if constexpr (!RMS) v[j][i] = j * LANES + lane < chunks ? v[j][i] - mean : 0.0f;
       sq = fmaf(v[j][i], v[j][i], sq);
     }
-  const float rstd = 1.0f / sqrtf(fmaf(row_reduce<LANES, SUM>(sq, lds, turn), inv_d, eps));
+  float ms = fmaf(row_reduce<LANES, SUM>(sq, lds, turn), inv_d, eps);
+  // Squares above the largest float, or near the least where eps is too: once more
+  // with the row times a power of 2, which leaves v / sqrt(ms) what it is.  (The
+  // lanes of a row agree, and a wave or a workgroup takes the branch as one.)
+  if (__any(!(ms >= 0x1p-100f && ms <= FLT_MAX))) {
+    const float by = ms > FLT_MAX ? 0x1p-80f : ms < 0x1p-100f ? 0x1p80f : 1.0f;
+    sq = 0.0f;
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[j][i] *= by;
+        sq = fmaf(v[j][i], v[j][i], sq);
+      }
+    ms = fmaf(row_reduce<LANES, SUM>(sq, lds, turn), inv_d, eps * by * by);
+  }
+  const float rstd = 1.0f / sqrtf(ms);
 #pragma unroll
   for (int j = 0; j < CH; ++j)
 #pragma unroll

@@ -7,7 +7,7 @@ import pytest
 from gpu_util import torch_cuda
 from paper_2605_01060_amd import surge as S
 from test_gpu_reader import (BF16, F32, block_norm, cross_call, cross_inputs,
-                             cross_reference, cu_of, gen, norm_inputs, norm_reference, within)
+                             cross_reference, cu_of, gen, norm64, norm_inputs, norm_reference, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -258,3 +258,31 @@ def test_block_norm_of_an_infinite_gate_over_a_beta_of_0(d):
     inf = ry.isinf()
     assert inf.sum() == 2 * M and torch.equal(y.double()[inf], ry[inf])
     within(y[~inf], ry[~inf], (BF16 * ry.abs() + 1.01 * ey)[~inf])
+
+
+@pytest.mark.parametrize("kind", [S.NORM_LAYER, S.NORM_RMS])
+@pytest.mark.parametrize("d", [8, 200, 384, 768, 2048, 3592, 8192])
+@pytest.mark.parametrize("power,eps", [(64, 1e-5), (100, 1e-5), (100, 0.0), (30, 0.0), (-40, 0.0), (-64, 0.0),
+                                       (-100, 0.0), (-120, 0.0)])
+def test_block_norm_of_rows_whose_squares_leave_the_floats(kind, d, power, eps):
+    """A norm without an eps that counts is the same of a row times a power of 2,
+    though the squares of some rows here are above the largest or below the
+    least float.  Rows of ordinary size beside them."""
+    torch = torch_cuda()
+    M, layer = 9, kind == S.NORM_LAYER
+    p = norm_inputs(M, d, layer, True, "none", True, d + kind)
+    by = torch.ones(M, 1, device="cuda")
+    by[::3], by[1::3] = 2.0 ** power, 2.0 ** (power // 2)
+    # (Times a power of 2 rounded again where a bf16 has fewer bits, below 2^-126.)
+    x, block = ((p[k].float() * by).bfloat16() for k in ("x", "block"))
+    far = torch.zeros_like(x)
+    exact = torch.zeros(M, d, dtype=torch.float64, device="cuda")
+    big = 2.0 ** 40  # the reference's eps counts for nothing here
+    z, n = (torch.empty(M, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    block_norm({**p, "x": x, "block": None, "post_gamma": None, "post_beta": None}, M, d, kind, 1.0, None, z,
+               eps=eps)
+    ref, tol = norm64(x.double() / by.double() * big, exact, layer, p["pre_gamma"], p["pre_beta"], d)
+    within(z, ref, BF16 * ref.abs() + 1.01 * tol)
+    block_norm({**p, "x": far, "block": block}, M, d, kind, 1.0, n, None, eps=eps)
+    ref, tol = norm64(block.double() / by.double() * big, exact, layer, p["post_gamma"], p["post_beta"], d)
+    within(n, ref, BF16 * ref.abs() + 1.01 * tol)
