@@ -156,7 +156,8 @@ surge_status surge_op_quantize_rows(int64_t M, int32_t K, const uint16_t* d_x, i
 
 /*
  * Linear layer in 8-bit integers with scales for each token and channel:
- *   y[m][n] = epi(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n]).
+ *   y[m][n] = epi(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n]),
+ * in fp32 from the exact sum on: times x_scale, times w_scale, plus bias.
  * d_x int8 [M, K]; d_x_scale fp32 [M]; d_w int8 [N, K] contiguous (out, in);
  * d_w_scale, d_bias fp32 [N], 16-byte aligned; epilogue as surge_op_linear (0
  * bias, 1 exact GELU, 2 + d_res, bf16 [M, N]); d_y bf16 [M, N].  The sum over
@@ -190,7 +191,8 @@ int32_t surge_op_linear_i8_tile(int64_t M, int32_t N, int32_t K, int32_t n_cus);
  * bf16 [M, d], the next block's input; d_zq int8 with d_zq_scale fp32 [M],
  * the same rows as surge_op_quantize_rows gives them, before a rounding to
  * bf16 (d_zq has d rounded up to a multiple of 128 columns).  Each output may
- * be NULL, not all.  z is made from y before its rounding to bf16.
+ * be NULL, not all.  z is made from y before its rounding to bf16; a row whose
+ * sum of features overflows fp32 has NaN in z under SURGE_NORM_LAYER.
  * NULL inputs: d_block (y = res_scale * x; then no post norm or gate),
  * d_post_gamma (no norm after the block), either beta (0; always NULL for
  * SURGE_NORM_RMS), d_gate, d_gate_rows (1).  d_pre_gamma is needed for z.
