@@ -258,6 +258,127 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
                                       void* d_workspace, int64_t workspace_bytes, uint16_t* d_out,
                                       int64_t ld_out, void* hip_stream);
 
+/*
+ * Operators of a decoder of answers: its keys and values in 4 bits, attention
+ * over them, and the check of tokens that a smaller model drafted.  Like the
+ * reader's they only enqueue, and can be captured; what changes from step to
+ * step (lengths, table, offsets) is read on the device when the call runs.
+ *
+ * A cache is pages of page_tokens (16, 32, 64, 128 or 256) consecutive
+ * positions of a sequence.  A page has surge_cache_page_bytes and holds, for
+ * every key head in turn,
+ *   the codes of its keys, page_tokens x d_head / 2 bytes, then of its values,
+ *   the scales of its keys, page_tokens x d_head / 32 bytes, then of its values.
+ * A code is a 4-bit float (sign, two bits of exponent, one of mantissa: 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 for 0 to 7), feature 2i in the low half of byte i; a scale is
+ * 2^(byte - 127) of 32 consecutive features, made and read with a byte from 25
+ * to 252, or 255 for NaN.  d_head is 32, 64 or 128.
+ *
+ * Sequence i's positions j are in page d_table[i ld_table + j / page_tokens].
+ * d_lengths [n_seqs] counts its positions, those that a call writes among them;
+ * below 0 counts as 0, beyond max_length as max_length.  Entries of positions
+ * beyond the length are not looked at.  An entry outside [0, n_pages) is no
+ * page: nothing is written there, and what is read there is NaN.  Pages may be
+ * shared by sequences, but two rows of one write must not have the same place.
+ *
+ * The rows of a call are packed as the texts of a SuperBatch: sequence i has
+ * rows d_cu[i] .. d_cu[i+1]-1 (device int32 [n_seqs+1], never decreasing, from
+ * 0) of n_rows in all, or n_rows / n_seqs each where d_cu is NULL.  They are its
+ * last positions: of n rows, row r is position length - n + r.  Rows of the
+ * matrices behind the last sequence are neither read nor written.
+ *
+ * d_pages 16-byte aligned; n_pages below 2^31; n_kv_heads at most 1024; n_seqs
+ * at most 2^20; ld_table at least max_length / page_tokens, rounded up;
+ * max_length and n_rows at most 2^30.  The struct is read by the call.
+ */
+typedef struct surge_kv_cache {
+  uint8_t* d_pages;
+  int64_t n_pages;
+  int32_t page_tokens, n_kv_heads, d_head, n_seqs;
+  const int32_t* d_table;
+  int64_t ld_table;
+  const int32_t* d_lengths;
+  int64_t max_length;
+} surge_kv_cache;
+
+/* Bytes of a page (host-only). */
+surge_status surge_cache_page_bytes(int32_t page_tokens, int32_t n_kv_heads, int32_t d_head,
+                                    int64_t* bytes);
+
+/*
+ * Rows of keys and values (bf16 [n_rows, n_kv_heads d_head], two column ranges
+ * of one projection's output, say) quantized and written to their positions.  Of
+ * 32 features with a = max(max |x|, 2^-100) the scale s is the least power of two
+ * with a <= 7 s, at most 2^125, and a code stands for the number nearest to x / s
+ * (ties to the even code, beyond 6 is 6): off by s at most, below 4 s by s / 2, below 2 s
+ * by s / 4.  32 features with an infinity or a NaN are marked as NaN.  Rows of negative
+ * positions (more rows than the sequence is long) are not written.
+ */
+surge_status surge_op_cache_write(const surge_kv_cache* cache, int64_t n_rows, const int32_t* d_cu,
+                                  const uint16_t* d_k, int64_t ld_k, const uint16_t* d_v, int64_t ld_v,
+                                  void* hip_stream);
+
+/*
+ * The reverse: what the codes of the rows' positions stand for, code times
+ * scale, exactly (a bf16).  Rows of negative positions are zeros.
+ */
+surge_status surge_op_cache_read(const surge_kv_cache* cache, int64_t n_rows, const int32_t* d_cu,
+                                 uint16_t* d_k, int64_t ld_k, uint16_t* d_v, int64_t ld_v,
+                                 void* hip_stream);
+
+/*
+ * Attention over the cache: out[t][h] = sum_k p_k v[k] / sum_k p_k, p_k =
+ * exp(scale q[t][h] . k[k]), over the positions k of t's sequence, with causal 1
+ * only those up to t's own; a row that sees none gives zeros.  n_heads query
+ * heads share the key heads in equal groups, as in cross attention, whose
+ * numerics these are: fp32 scores, maxima, sums and outputs, each p_k rounded to
+ * bf16 for its product with v; a row of which a score is a NaN, the largest
+ * overflows or none is above -infinity gives NaN.  A key or value with
+ * features marked as NaN makes NaN the rows of its heads that see it; what rows
+ * don't see, or what stands behind a sequence's length, does not reach them.
+ * d_q, d_out bf16 [n_rows, n_heads d_head]; max_rows: at least the rows of each
+ * sequence (of one with more, the rows from max_rows on are left as they were),
+ * max_rows n_heads at most 2^30; n_heads at most 1024; scale positive, below
+ * 2^127.  max_length and max_rows cut the call into units, so in a captured
+ * call they are the bounds of its replays.  d_workspace as in cross attention,
+ * of surge_cache_attention_workspace bytes for the same cache, max_rows and
+ * n_heads.  d_out must not overlap an input.
+ */
+surge_status surge_cache_attention_workspace(const surge_kv_cache* cache, int64_t max_rows,
+                                             int32_t n_heads, int64_t* bytes);
+surge_status surge_op_cache_attention(const surge_kv_cache* cache, int64_t n_rows, const int32_t* d_cu,
+                                      int64_t max_rows, int32_t n_heads, int32_t causal, float scale,
+                                      const uint16_t* d_q, int64_t ld_q, void* d_workspace,
+                                      int64_t workspace_bytes, uint16_t* d_out, int64_t ld_out,
+                                      void* hip_stream);
+
+/*
+ * Drafted tokens against the target's probabilities, from given random numbers
+ * u in [0, 1).  Sequence i has n = d_n_drafts[i] drafts (clamped to [0,
+ * max_drafts]; max_drafts each where d_n_drafts is NULL), x_j = d_drafts[i
+ * max_drafts + j], with the drafting model's probabilities q_j in row i
+ * max_drafts + j of d_q, and the target's p_j, j = 0 .. n, in row i (max_drafts +
+ * 1) + j of d_p.  Draft j is accepted where u_j q_j(x_j) < p_j(x_j) and all before
+ * it are (a draft that is no token of the vocabulary is not).  After the accepted
+ * ones one more token is drawn, the least v with sum_{w <= v} r(w) > u_last
+ * sum_w r(w), where r is max(p_a - q_a, 0) of the first rejected draft a, or p_n
+ * after n accepted ones.  Without d_q drafts are certain: q_j is 1 at x_j.  Where
+ * nothing of r is above 0, r is p_a.  Comparisons and sums are in 64 bits; a
+ * probability that is not above 0 (NaN too) counts as 0, and a row whose sum is
+ * infinite or 0 gives token -1.
+ * d_p, d_q fp32 rows of vocab (at most 2^22) probabilities, ld_p and ld_q apart;
+ * d_u fp32 [n_seqs, max_drafts + 1], u_j at j, u_last in the last column.
+ * Outputs: d_tokens int32 [n_seqs, max_drafts + 1], the accepted drafts, the drawn
+ * token, then -1; d_accepted int32 [n_seqs].  max_drafts at most 1024, n_seqs at
+ * most 2^20.  d_workspace as above, of surge_verify_workspace bytes.
+ */
+surge_status surge_verify_workspace(int64_t n_seqs, int32_t vocab, int64_t* bytes);
+surge_status surge_op_verify_drafts(int64_t n_seqs, int32_t max_drafts, int32_t vocab,
+                                    const int32_t* d_n_drafts, const int32_t* d_drafts, const float* d_p,
+                                    int64_t ld_p, const float* d_q, int64_t ld_q, const float* d_u,
+                                    void* d_workspace, int64_t workspace_bytes, int32_t* d_tokens,
+                                    int32_t* d_accepted, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

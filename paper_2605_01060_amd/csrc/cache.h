@@ -1,0 +1,75 @@
+// Launchers of the operators of a decoder: its keys and values in 4 bits,
+// attention over them, and the check of drafted tokens.  The caller has
+// checked the arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace surge {
+
+// Pages of tokens, see surge_kv_cache.  A page holds for every key head, in
+// turn: the codes of its keys [tokens, d_head / 2 bytes], of its values, the
+// scales of its keys [tokens, d_head / 32 bytes], of its values.
+struct CacheView {
+  uint8_t* pages;
+  int64_t n_pages, page_bytes;
+  int page_shift, n_kv_heads, n_seqs, max_length;
+  const int32_t* table;
+  int64_t ld_table;
+  const int32_t* lengths;
+};
+
+// The rows of a call: sequence i has rows cu[i] .. cu[i+1]-1, or `each` rows
+// where cu is NULL, of n_rows in all.  They are its last positions.
+struct CacheRows {
+  const int32_t* cu;
+  int n_rows, each;
+};
+
+struct CacheStore {
+  CacheView c;
+  CacheRows r;
+  uint16_t *k, *v;  // read by a write, written by a read
+  int64_t ld_k, ld_v;
+};
+hipError_t launch_cache_write(const CacheStore& a, int d_head, hipStream_t stream);
+hipError_t launch_cache_read(const CacheStore& a, int d_head, hipStream_t stream);
+
+struct CacheAttention {
+  CacheView c;
+  CacheRows r;
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t ld_q, ld_out;
+  int group, max_rows;
+  bool causal;
+  float scale_log2;   // scale * log2(e)
+  // Of cache_attention_shape.
+  int tile_rows, tiles, splits, chunk;
+  float2* part_ml;    // [sequence, tile, key head, split, row] (maximum in log2 units, sum)
+  float* part_o;      // [the same, d_head]
+};
+
+// How a call is cut into units: tiles of tile_rows rows (query * group + head
+// of the group) of each sequence, and their keys into at most `splits` ranges
+// of `chunk` keys.
+struct CacheShape {
+  int tile_rows;
+  int64_t tiles, splits, chunk;
+};
+CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_heads, int group, int d_head,
+                                 int64_t max_length, int n_cus);
+hipError_t launch_cache_attention(const CacheAttention& a, int d_head, hipStream_t stream);
+
+struct VerifyDrafts {
+  int max_drafts, vocab;
+  const int32_t *n_drafts, *drafts;  // n_drafts NULL: max_drafts each
+  const float *p, *q;                // q NULL: drafts of probability 1
+  int64_t ld_p, ld_q;
+  const float* u;
+  int32_t *tokens, *accepted;
+};
+hipError_t launch_verify_drafts(int64_t n_seqs, const VerifyDrafts& a, hipStream_t stream);
+
+}  // namespace surge

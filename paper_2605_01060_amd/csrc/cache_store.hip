@@ -1,0 +1,202 @@
+// Keys and values written to a cache's pages in 4 bits and read back (gfx950).
+//
+// Every 32 values of a row have a scale s = 2^e, the least with a <= 7 s for
+// a = max(max |x|, 2^-100) (at most 2^125), and the 4-bit float nearest to x / s
+// each (+-0, 0.5, 1, 1.5, 2, 3, 4, 6; ties to the even code; what rounds beyond 6
+// is 6, off by s at most like the values between 4 and 6).  With a scale of a
+// power of two both steps are exact but for that one rounding, and a code times
+// its scale is a bf16: reading back rounds nothing.
+//
+// A wave takes 16 rows of one key head: 8 features a lane, so that it reads 16
+// bytes a lane, 64 to 256 of a row together, and writes the codes of
+// neighbouring tokens, which lie behind each other in a page, together too.
+#include "cache_device.h"
+
+namespace surge {
+namespace {
+
+constexpr int ROWS = 16;  // of a wave
+
+// Which sequence and position a row is.
+struct RowPlace {
+  int seq, pos, length;  // seq < 0: a row of no sequence
+};
+
+// The places of rows t0 + r (r < ROWS, one per lane).  cu is searched by 64
+// lanes at a time, then the boundaries from there on are walked in registers.
+// Offsets that decrease give places within bounds, whatever they are.
+__device__ __forceinline__ RowPlace place_of(const CacheView& c, const CacheRows& rows, int t0, int r) {
+  RowPlace at = {-1, 0, 0};
+  const int t = t0 + r;
+  if (rows.cu == nullptr) {
+    if (t < rows.n_rows) {
+      at.seq = t / rows.each;
+      at.length = length_of(c, at.seq);
+      at.pos = at.length - (at.seq + 1) * rows.each + t;
+    }
+    return at;
+  }
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = c.n_seqs;  // the last i with cu[i] <= t0 is in [lo, hi)
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64;
+    const int i = lo + lane * step;
+    const int n = __popcll(__ballot(i < hi && rows.cu[min(i, c.n_seqs)] <= t0));
+    if (n > 0) lo += (n - 1) * step;
+    hi = min(lo + step, hi);
+  }
+  int seq = lo, end = 0;
+  bool found = false;
+  const int first = rows.cu[lo];
+  for (int base = lo + 1; base <= c.n_seqs; base += 64) {
+    const int bounds = rows.cu[min(base + lane, c.n_seqs)];
+    const int n = min(64, c.n_seqs - base + 1);
+    for (int e = 0; e < n; ++e) {
+      const int bound = __builtin_amdgcn_readlane(bounds, e);
+      if (!found && t >= bound) seq = base + e;
+      if (!found && t < bound) {
+        found = true;
+        end = bound;
+      }
+      if (bound >= t0 + ROWS) break;
+    }
+    if (__all(found)) break;
+  }
+  if (found && t >= first && t < rows.n_rows) {
+    at.seq = seq;
+    at.length = length_of(c, seq);
+    at.pos = at.length - end + t;
+  }
+  return at;
+}
+
+// The page's part of key head `head` that holds position pos, or NULL where
+// the table's entry is no page.
+template <int DH>
+__device__ __forceinline__ uint8_t* page_of(const CacheView& c, int seq, int pos, int head) {
+  const int page = c.table[seq * c.ld_table + (pos >> c.page_shift)];
+  if (page < 0 || page >= c.n_pages) return nullptr;
+  return c.pages + page * c.page_bytes + head * PageLayout<DH>::head_bytes(c.page_shift);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) void cache_write_kernel(CacheStore a) {
+  using L = PageLayout<DH>;
+  constexpr int PER = DH / 8;       // lanes of a row
+  constexpr int STEP = 64 / PER;    // rows of a wave at a time
+  constexpr int N = ROWS / STEP;
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = (int)(wave % a.c.n_kv_heads);
+  const int64_t group = wave / a.c.n_kv_heads;
+  if (group * ROWS >= a.r.n_rows) return;
+  const int t0 = (int)group * ROWS, piece = lane % PER;
+  uint4 x[2][N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int64_t t = min(t0 + n * STEP + lane / PER, a.r.n_rows - 1);
+    x[0][n] = *reinterpret_cast<const uint4*>(a.k + t * a.ld_k + head * DH + piece * 8);
+    x[1][n] = *reinterpret_cast<const uint4*>(a.v + t * a.ld_v + head * DH + piece * 8);
+  }
+  const RowPlace mine = place_of(a.c, a.r, t0, lane % ROWS);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int from = n * STEP + lane / PER;
+    const int seq = __shfl(mine.seq, from), pos = __shfl(mine.pos, from);
+    uint8_t* const page = seq < 0 || pos < 0 ? nullptr : page_of<DH>(a.c, seq, pos, head);
+    const int slot = pos & ((1 << a.c.page_shift) - 1);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const uint32_t xs[4] = {x[w][n].x, x[w][n].y, x[w][n].z, x[w][n].w};
+      // Largest magnitude, as bits (of infinities and NaN the largest).
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        most = max(most, xs[i] << 16 & 0x7fff0000u);
+        most = max(most, xs[i] & 0x7fff0000u);
+      }
+      most = max(most, (uint32_t)__shfl_xor((int)most, 1));
+      most = max(most, (uint32_t)__shfl_xor((int)most, 2));
+      // With a = 1.f 2^E: e = E - 2 where 1.f <= 1.75, else E - 1.
+      uint32_t byte = (max(most, 0x0d800000u) + 0x1fffffu >> 23) - 2;
+      byte = most >= 0x7f800000u ? NAN_SCALE : min(byte, 252u);
+      const float scale = scale_of(byte);
+      uint32_t codes = 0;
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[0]), scale, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[1]), scale, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[2]), scale, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[3]), scale, 3);
+      if (page) {
+        *reinterpret_cast<uint32_t*>(page + L::codes(a.c.page_shift, slot, w) + piece * 4) = codes;
+        if (piece % 4 == 0) page[L::scales(a.c.page_shift, slot, w) + piece / 4] = (uint8_t)byte;
+      }
+    }
+  }
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheStore a) {
+  using L = PageLayout<DH>;
+  constexpr int PER = DH / 8, STEP = 64 / PER, N = ROWS / STEP;
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = (int)(wave % a.c.n_kv_heads);
+  const int64_t group = wave / a.c.n_kv_heads;
+  if (group * ROWS >= a.r.n_rows) return;
+  const int t0 = (int)group * ROWS, piece = lane % PER;
+  const RowPlace mine = place_of(a.c, a.r, t0, lane % ROWS);
+  uint32_t codes[N][2], bytes[N][2];
+  bool row[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int from = n * STEP + lane / PER;
+    const int seq = __shfl(mine.seq, from), pos = __shfl(mine.pos, from);
+    row[n] = seq >= 0;
+    codes[n][0] = codes[n][1] = 0;
+    bytes[n][0] = bytes[n][1] = pos < 0 ? 1 : NAN_SCALE;  // zeros, or no page
+    if (row[n] && pos >= 0) {
+      const uint8_t* const page = page_of<DH>(a.c, seq, pos, head);
+      const int slot = pos & ((1 << a.c.page_shift) - 1);
+      if (page)
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          codes[n][w] = *reinterpret_cast<const uint32_t*>(page + L::codes(a.c.page_shift, slot, w) + piece * 4);
+          bytes[n][w] = page[L::scales(a.c.page_shift, slot, w) + piece / 4];
+        }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int64_t t = t0 + n * STEP + lane / PER;
+    if (!row[n]) continue;
+    *reinterpret_cast<u32x4*>(a.k + t * a.ld_k + head * DH + piece * 8) =
+        __builtin_bit_cast(u32x4, decode8(codes[n][0], scale_of(bytes[n][0])));
+    *reinterpret_cast<u32x4*>(a.v + t * a.ld_v + head * DH + piece * 8) =
+        __builtin_bit_cast(u32x4, decode8(codes[n][1], scale_of(bytes[n][1])));
+  }
+}
+
+unsigned blocks(const CacheStore& a) {
+  const int64_t waves = ((int64_t)a.r.n_rows + ROWS - 1) / ROWS * a.c.n_kv_heads;
+  return (unsigned)((waves + 3) / 4);
+}
+
+}  // namespace
+
+hipError_t launch_cache_write(const CacheStore& a, int d_head, hipStream_t stream) {
+  const dim3 grid(blocks(a));
+  if (d_head == 32) hipLaunchKernelGGL(cache_write_kernel<32>, grid, dim3(256), 0, stream, a);
+  if (d_head == 64) hipLaunchKernelGGL(cache_write_kernel<64>, grid, dim3(256), 0, stream, a);
+  if (d_head == 128) hipLaunchKernelGGL(cache_write_kernel<128>, grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_read(const CacheStore& a, int d_head, hipStream_t stream) {
+  const dim3 grid(blocks(a));
+  if (d_head == 32) hipLaunchKernelGGL(cache_read_kernel<32>, grid, dim3(256), 0, stream, a);
+  if (d_head == 64) hipLaunchKernelGGL(cache_read_kernel<64>, grid, dim3(256), 0, stream, a);
+  if (d_head == 128) hipLaunchKernelGGL(cache_read_kernel<128>, grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace surge

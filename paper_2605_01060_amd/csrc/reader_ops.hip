@@ -3,25 +3,15 @@
 #include <math.h>
 
 #include <algorithm>
-#include <atomic>
 #include <exception>
 #include <new>
 
+#include "checks.h"
 #include "cross.h"
-#include "internal.h"
-#include "kernels.h"
 #include "reader.h"
 #include "surge_ops.h"
 
 using namespace surge;
-
-#define HIP_TRY(expr)                                                                     \
-  do {                                                                                    \
-    hipError_t e_ = (expr);                                                               \
-    if (e_ != hipSuccess)                                                                 \
-      return fail(e_ == hipErrorOutOfMemory ? SURGE_ERR_OUT_OF_MEMORY : SURGE_ERR_DEVICE, \
-                  "%s failed: %s", #expr, hipGetErrorString(e_));                         \
-  } while (0)
 
 struct surge_cross_plan {
   int device = 0;
@@ -35,44 +25,6 @@ struct surge_cross_plan {
 };
 
 namespace {
-
-// Row strides are bounded so that the offset of a row within a tile or key
-// block fits 32 bits.
-constexpr int64_t kMaxStride = 1 << 22;
-
-bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
-
-// A matrix of `rows` x `cols` elements, `ld` apart, read or written 16 bytes
-// at a time.
-surge_status check_matrix(const char* name, const void* p, int64_t cols, int64_t ld, int unit) {
-  if (!p) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s is NULL", name);
-  if (!aligned(p, 16)) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s must be 16-byte aligned", name);
-  if (ld < cols || ld > kMaxStride || ld % unit)
-    return fail(SURGE_ERR_INVALID_ARGUMENT,
-                "row stride %lld of %s: a multiple of %d in [%lld, %lld] is needed", (long long)ld,
-                name, unit, (long long)cols, (long long)kMaxStride);
-  return SURGE_OK;
-}
-
-surge_status check_vector(const char* name, const void* p, bool needed) {
-  if (!p && needed) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s is NULL", name);
-  if (!aligned(p, 16)) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s must be 16-byte aligned", name);
-  return SURGE_OK;
-}
-
-// An output in the place of an input (`over` says whether it may be, with the
-// same stride) or of another output.
-surge_status check_place(const char* name, const void* p, int64_t ld, const char* other, const void* q,
-                         int64_t ld_other, bool over) {
-  if (!p || p != q || (over && ld == ld_other)) return SURGE_OK;
-  return fail(SURGE_ERR_INVALID_ARGUMENT, over ? "%s over %s needs its stride" : "%s is %s", name, other);
-}
-
-surge_status check_rows(int64_t M) {
-  if (M < 0 || M > (int64_t)INT32_MAX)
-    return fail(SURGE_ERR_INVALID_ARGUMENT, "M=%lld outside [0, 2^31)", (long long)M);
-  return SURGE_OK;
-}
 
 // Rows of queries and of keys are counted in 32 bits, a block of them beyond
 // the last one too.
@@ -88,33 +40,6 @@ surge_status check_offsets(const char* name, int64_t n, const int64_t* cu) {
   if (cu[n] > kMostRows) return fail(SURGE_ERR_INVALID_ARGUMENT, "%s: too many rows", name);
   return SURGE_OK;
 }
-
-// The current device and its compute units, asked for once a device, and that
-// the stream is one of this device's.
-surge_status current_device(hipStream_t stream, int* dev, int* n_cus) {
-  constexpr int kMaxDevices = 64;
-  static std::atomic<int> known[kMaxDevices];
-  HIP_TRY(hipGetDevice(dev));
-  if (stream) {
-    int own = 0;
-    HIP_TRY(hipStreamGetDevice(stream, &own));
-    if (own != *dev)
-      return fail(SURGE_ERR_INVALID_ARGUMENT, "a stream of device %d, the current one is %d", own, *dev);
-  }
-  if (*dev < 0 || *dev >= kMaxDevices)
-    return fail(SURGE_ERR_DEVICE, "device index %d outside [0, %d)", *dev, kMaxDevices);
-  *n_cus = known[*dev].load(std::memory_order_relaxed);
-  if (*n_cus > 0) return SURGE_OK;
-  HIP_TRY(resolve_cus(n_cus));
-  known[*dev].store(*n_cus, std::memory_order_relaxed);
-  return SURGE_OK;
-}
-
-#define CHECK(expr)                     \
-  do {                                  \
-    const surge_status st_ = (expr);    \
-    if (st_ != SURGE_OK) return st_;    \
-  } while (0)
 
 int64_t part_rows(const surge_cross_plan* p) { return p->n_parts * p->n_kv_heads * 32; }
 int64_t workspace_bytes(const surge_cross_plan* p) {

@@ -114,6 +114,15 @@ _SIGNATURES = {
     "surge_cross_plan_info": ([_P, _P, _P, _P], _I32),
     "surge_op_cross_attention": ([_P, _P, _I64, _P, _I64, _P, _I64, _P, ctypes.c_float, _P, _I64,
                                   _P, _I64, _P], _I32),
+    "surge_cache_page_bytes": ([_I32, _I32, _I32, _P], _I32),
+    "surge_op_cache_write": ([_P, _I64, _P, _P, _I64, _P, _I64, _P], _I32),
+    "surge_op_cache_read": ([_P, _I64, _P, _P, _I64, _P, _I64, _P], _I32),
+    "surge_cache_attention_workspace": ([_P, _I64, _I32, _P], _I32),
+    "surge_op_cache_attention": ([_P, _I64, _P, _I64, _I32, _I32, ctypes.c_float, _P, _I64, _P, _I64,
+                                  _P, _I64, _P], _I32),
+    "surge_verify_workspace": ([_I64, _I32, _P], _I32),
+    "surge_op_verify_drafts": ([_I64, _I32, _I32, _P, _P, _P, _I64, _P, _I64, _P, _P, _I64, _P, _P,
+                                _P], _I32),
 }
 
 
@@ -465,6 +474,73 @@ class CrossPlan:
             self.close()
         except Exception:
             pass
+
+
+# Operators of a decoder of answers (asynchronous) -----------------------------
+
+class KVCache(ctypes.Structure):
+    """A surge_kv_cache: pages, table and lengths are device tensors (kept alive
+    by this object) or addresses, read by the calls as they are then."""
+
+    _fields_ = [("d_pages", _P), ("n_pages", _I64), ("page_tokens", _I32), ("n_kv_heads", _I32),
+                ("d_head", _I32), ("n_seqs", _I32), ("d_table", _P), ("ld_table", _I64),
+                ("d_lengths", _P), ("max_length", _I64)]
+
+    def __init__(self, pages, n_pages: int, page_tokens: int, n_kv_heads: int, d_head: int, table,
+                 ld_table: int, n_seqs: int, lengths, max_length: int):
+        super().__init__(_dev(pages), n_pages, page_tokens, n_kv_heads, d_head, n_seqs, _dev(table),
+                         ld_table, _dev(lengths), max_length)
+        self.kept = (pages, table, lengths)
+
+
+def surge_cache_page_bytes(page_tokens: int, n_kv_heads: int, d_head: int) -> int:
+    v = ctypes.c_int64(0)
+    _check(lib().surge_cache_page_bytes(page_tokens, n_kv_heads, d_head, ctypes.byref(v)))
+    return v.value
+
+
+def surge_op_cache_write(cache: KVCache, n_rows, d_cu, d_k, ld_k, d_v, ld_v, stream=None):
+    _check(lib().surge_op_cache_write(ctypes.byref(cache), n_rows, _dev(d_cu), _dev(d_k), ld_k,
+                                      _dev(d_v), ld_v, _stream(stream)))
+
+
+def surge_op_cache_read(cache: KVCache, n_rows, d_cu, d_k, ld_k, d_v, ld_v, stream=None):
+    _check(lib().surge_op_cache_read(ctypes.byref(cache), n_rows, _dev(d_cu), _dev(d_k), ld_k,
+                                     _dev(d_v), ld_v, _stream(stream)))
+
+
+def surge_cache_attention_workspace(cache: KVCache, max_rows: int, n_heads: int) -> int:
+    """Bytes of workspace that a call needs on the current device."""
+    v = ctypes.c_int64(0)
+    _check(lib().surge_cache_attention_workspace(ctypes.byref(cache), max_rows, n_heads,
+                                                 ctypes.byref(v)))
+    return v.value
+
+
+def surge_op_cache_attention(cache: KVCache, n_rows, d_cu, max_rows, n_heads, causal, scale, d_q, ld_q,
+                             workspace, d_out, ld_out, stream=None):
+    """workspace: a device tensor of at least surge_cache_attention_workspace
+    bytes (None where that is 0)."""
+    _check(lib().surge_op_cache_attention(ctypes.byref(cache), n_rows, _dev(d_cu), max_rows, n_heads,
+                                          int(causal), scale, _dev(d_q), ld_q, _dev(workspace),
+                                          0 if workspace is None else workspace.nbytes, _dev(d_out),
+                                          ld_out, _stream(stream)))
+
+
+def surge_verify_workspace(n_seqs: int, vocab: int) -> int:
+    v = ctypes.c_int64(0)
+    _check(lib().surge_verify_workspace(n_seqs, vocab, ctypes.byref(v)))
+    return v.value
+
+
+def surge_op_verify_drafts(n_seqs, max_drafts, vocab, d_n_drafts, d_drafts, d_p, ld_p, d_q, ld_q, d_u,
+                           workspace, d_tokens, d_accepted, stream=None):
+    """workspace: a device tensor of at least surge_verify_workspace bytes (None
+    where that is 0)."""
+    _check(lib().surge_op_verify_drafts(n_seqs, max_drafts, vocab, _dev(d_n_drafts), _dev(d_drafts),
+                                        _dev(d_p), ld_p, _dev(d_q), ld_q, _dev(d_u), _dev(workspace),
+                                        0 if workspace is None else workspace.nbytes, _dev(d_tokens),
+                                        _dev(d_accepted), _stream(stream)))
 
 
 # Convenience: an encoder object over device-resident inputs ----------------

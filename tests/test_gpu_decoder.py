@@ -1,0 +1,807 @@
+"""The decoder's operators on the GPU against their definitions in 64 bits:
+keys and values written to a cache in 4 bits and read back, attention over it,
+the check of drafted tokens, and the three together.
+
+What a cache holds is compared bit by bit.  Attention's tolerance counts
+roundings: one to bf16 is off by at most BF16 = 2^-8 of the value, one in fp32
+by F32 = 2^-24.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from gpu_util import torch_cuda
+from paper_2605_01060_amd import surge as S
+from test_gpu_reader import BF16, F32, gen, randn, strided, within
+
+pytestmark = pytest.mark.gpu
+
+VALUES = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+TINY = 2.0 ** -100
+
+
+def dev(x, dtype=np.int32):
+    return torch_cuda().from_numpy(np.ascontiguousarray(x, dtype)).cuda()
+
+
+def cu_of(counts):
+    return dev(np.concatenate([[0], np.cumsum(counts)]))
+
+
+def quantized(x):
+    """Codes [T, w] 0..15 and scale bytes [T, w / 32] of bf16 rows, in 64 bits."""
+    torch = torch_cuda()
+    x = x.double().view(len(x), -1, 32)
+    a = x.abs().amax(2, keepdim=True)
+    marked = ~torch.isfinite(a)
+    a = torch.where(marked, 1.0, a.clamp_min(TINY))
+    e = torch.ceil(torch.log2(a / 7)).clamp_max(125)
+    y = x.abs() / torch.exp2(e)
+    code = torch.zeros(x.shape, dtype=torch.int64, device=x.device)
+    for i in range(7):  # nearest, ties to the even code
+        middle = (VALUES[i] + VALUES[i + 1]) / 2
+        code += (y > middle) | ((y == middle) & (i % 2 == 1))
+    code += 8 * torch.signbit(x)
+    byte = torch.where(marked, 255, e.long() + 127)
+    return code.flatten(1), byte[..., 0]
+
+
+def values(code, byte):
+    """What codes [.., w] and scale bytes [.., w / 32] stand for, in 64 bits."""
+    torch = torch_cuda()
+    v = torch.tensor(VALUES + [-x for x in VALUES], dtype=torch.float64, device=code.device)[code]
+    scale = torch.where(byte == 255, math.nan, torch.exp2(byte.double() - 127))
+    return (v.unflatten(-1, (-1, 32)) * scale[..., None]).flatten(-2)
+
+
+class Cache:
+    """Pages with random places for sequences of the given lengths, filled with
+    bytes that stand for NaN (or `fill`) until something is written."""
+
+    def __init__(self, lengths, page, hk, dh, seed, fill=255, room=0, spare=3):
+        torch = torch_cuda()
+        self.lengths_np, self.page, self.hk, self.dh = np.asarray(lengths, np.int64), page, hk, dh
+        need = -(-(self.lengths_np + room) // page)
+        total = int(need.sum())
+        self.n_pages = total + spare
+        rng = np.random.default_rng(seed)
+        perm = rng.permutation(self.n_pages)[:total]
+        self.width = max(int(need.max(initial=0)), 1) + 2
+        self.table_np = np.full((len(need), self.width), -7, np.int64)
+        self.table_np[np.arange(self.width) < need[:, None]] = perm
+        self.bytes = S.surge_cache_page_bytes(page, hk, dh)
+        self.pages = torch.full((self.n_pages, self.bytes), fill, dtype=torch.uint8, device="cuda")
+        self.table, self.lengths = dev(self.table_np), dev(self.lengths_np)
+        self.max_length = int((self.lengths_np + room).max(initial=0))
+        self.desc = S.KVCache(self.pages, self.n_pages, page, hk, dh, self.table, self.width, len(need),
+                              self.lengths, self.max_length)
+
+    def fields(self, pages=None):
+        """Codes of keys, of values, scales of keys, of values, as views."""
+        body = (self.pages if pages is None else pages).view(self.n_pages, self.hk, -1)
+        out, at = [], 0
+        for width in (self.dh // 2, self.dh // 2, self.dh // 32, self.dh // 32):
+            out.append(body[:, :, at:at + self.page * width].unflatten(2, (self.page, width)))
+            at += self.page * width
+        assert at == body.shape[2]
+        return out
+
+    def put(self, seq, pos, k, v, pages=None):
+        """Rows of keys and values [T, hk dh] at positions, by the definition."""
+        torch = torch_cuda()
+        page = torch.from_numpy(self.table_np[seq, np.asarray(pos) // self.page]).cuda()
+        slot = torch.from_numpy(np.asarray(pos) % self.page).cuda()
+        f = self.fields(pages)
+        for w, x in enumerate((k, v)):
+            code, byte = quantized(x)
+            code = code.view(len(x), self.hk, self.dh)
+            f[w][page, :, slot] = (code[..., ::2] + 16 * code[..., 1::2]).to(torch.uint8)
+            f[w + 2][page, :, slot] = byte.view(len(x), self.hk, -1).to(torch.uint8)
+
+    def fill(self, seed, scale=1.0):
+        """Every sequence's positions, and the values that they stand for."""
+        torch = torch_cuda()
+        g = gen(seed)
+        self.held = []
+        for i, n in enumerate(self.lengths_np):
+            k, v = ((scale * randn(g, int(n), self.hk * self.dh)).bfloat16() for _ in range(2))
+            if n:
+                self.put(i, np.arange(n), k, v)
+            self.held.append([values(*quantized(x)).view(int(n), self.hk, self.dh) if n else
+                              torch.zeros(0, self.hk, self.dh, dtype=torch.float64, device="cuda")
+                              for x in (k, v)])
+        return self
+
+
+def places(lengths, rows):
+    """Sequence and position of each row, some of them negative."""
+    seq = np.repeat(np.arange(len(rows)), rows)
+    pos = np.concatenate([np.arange(n - r, n) for n, r in zip(lengths, rows)]) if len(rows) else seq
+    return seq, pos.astype(np.int64)
+
+
+# ---------------------------------------------------------------------------
+# Written and read back
+# ---------------------------------------------------------------------------
+
+LENGTHS = [5, 0, 1, 16, 17, 40, 3, 64, 100, 33, 0, 2, 300, 15]
+ROWS = [5, 0, 1, 3, 17, 1, 7, 40, 0, 33, 2, 0, 129, 1]  # two sequences have more rows than positions
+
+
+@pytest.mark.parametrize("page,hk,dh", [(16, 1, 32), (16, 16, 64), (32, 3, 64), (64, 2, 128), (128, 5, 32),
+                                        (256, 1, 128), (32, 12, 64), (64, 8, 128)])
+@pytest.mark.parametrize("uniform", [0, 1, 3])
+def test_write_and_read(page, hk, dh, uniform):
+    torch = torch_cuda()
+    rows = [uniform] * len(LENGTHS) if uniform else ROWS
+    c = Cache(LENGTHS, page, hk, dh, page + hk, fill=0xAB)
+    g, n, w = gen(dh + uniform), sum(rows), hk * dh
+    k, v = ((randn(g, n + 2, w) * torch.exp2(6 * randn(g, n + 2, 1))).bfloat16() for _ in range(2))
+    (ks, _), (vs, _) = strided(k, 8), strided(v, 24)
+    cu = None if uniform else cu_of(rows)
+    want = c.pages.clone()
+    seq, pos = places(LENGTHS, rows)
+    on = pos >= 0
+    c.put(seq[on], pos[on], k[:n][torch.from_numpy(on).cuda()], v[:n][torch.from_numpy(on).cuda()], want)
+    stream = torch.cuda.current_stream()
+    S.surge_op_cache_write(c.desc, n, cu, ks, w + 8, vs, w + 24, stream)
+    assert torch.equal(c.pages, want)  # and nothing beside the rows' places
+    out = [torch.full((n + 2, w + 16), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    S.surge_op_cache_read(c.desc, n, cu, out[0], w + 16, out[1], w + 16, stream)
+    for x, o in ((k, out[0]), (v, out[1])):
+        ref = values(*quantized(x[:n]))
+        ref[torch.from_numpy(~on).cuda()] = 0
+        assert torch.equal(o[:n, :w].double(), ref)
+        assert (o[n:] == 7).all() and (o[:, w:] == 7).all()
+
+
+def test_write_of_rows_behind_the_last_sequence():
+    """Offsets that end before n_rows: the rows behind stay as they were."""
+    torch = torch_cuda()
+    c = Cache([40, 50], 16, 2, 64, 1, fill=0xAB)
+    g = gen(1)
+    k, v = (randn(g, 90, 128).bfloat16() for _ in range(2))
+    cu = dev([0, 10, 31])
+    want = c.pages.clone()
+    seq, pos = places([40, 50], [10, 21])
+    c.put(seq, pos, k[:31], v[:31], want)
+    S.surge_op_cache_write(c.desc, 90, cu, k, 128, v, 128)
+    assert torch.equal(c.pages, want)
+    out = [torch.full((90, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    S.surge_op_cache_read(c.desc, 90, cu, out[0], 128, out[1], 128)
+    assert torch.equal(out[0][:31].double(), values(*quantized(k[:31])))
+    assert (out[0][31:] == 7).all() and (out[1][31:] == 7).all()
+
+
+@pytest.mark.parametrize("seqs,empty", [(3000, False), (5000, True), (64, False), (65, True), (1, False)])
+def test_write_and_read_of_many_sequences(seqs, empty):
+    """Rows find their sequence among many, hundreds of empty ones between."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(seqs)
+    rows = rng.integers(0, 9, seqs)
+    if empty:
+        rows[rng.random(seqs) < 0.9] = 0
+        rows[10:min(seqs, 400)] = 0
+    rows[-1] = 3
+    lengths = rows + rng.integers(0, 20, seqs)
+    c = Cache(lengths, 16, 1, 32, seqs, fill=0xAB)
+    g, n = gen(seqs), int(rows.sum())
+    k, v = (randn(g, n, 32).bfloat16() for _ in range(2))
+    want = c.pages.clone()
+    c.put(*places(lengths, rows), k, v, want)
+    S.surge_op_cache_write(c.desc, n, cu_of(rows), k, 32, v, 32)
+    assert torch.equal(c.pages, want)
+    out = [torch.empty_like(k) for _ in range(2)]
+    S.surge_op_cache_read(c.desc, n, cu_of(rows), out[0], 32, out[1], 32)
+    assert torch.equal(out[0].double(), values(*quantized(k)))
+    assert torch.equal(out[1].double(), values(*quantized(v)))
+
+
+def test_write_of_every_bf16():
+    """Every finite bf16 as the largest of its 32 and beside larger ones."""
+    torch = torch_cuda()
+    bits = torch.arange(65536, device="cuda").to(torch.int16).view(torch.bfloat16)
+    x = bits[torch.isfinite(bits)]
+    rows = x[:, None].repeat(1, 32)
+    rows[:, 1:] *= torch.rand(31, generator=gen(1), device="cuda").bfloat16()
+    rows[::2, 7] = (rows[::2, 0].float() * 13).clamp(-3e38, 3e38).bfloat16()
+    n = len(rows) // 16 * 16
+    k, v = rows[:n].view(n // 16, 512), rows[:n].flip(0).view(n // 16, 512)
+    c = Cache([len(k)], 64, 16, 32, 1)
+    S.surge_op_cache_write(c.desc, len(k), None, k, 512, v, 512)
+    out = [torch.empty_like(k) for _ in range(2)]
+    S.surge_op_cache_read(c.desc, len(k), None, out[0], 512, out[1], 512)
+    for a, o in ((k, out[0]), (v, out[1])):
+        ref = values(*quantized(a))
+        assert torch.equal(o.double(), ref) and torch.isfinite(o).all()
+        # As documented: off by the scale at most.
+        b = a.double().view(-1, 32)
+        assert ((ref.view(-1, 32) - b).abs() <= b.abs().amax(1, keepdim=True).clamp_min(TINY) * (2 / 7)).all()
+
+
+def test_write_marks_what_is_not_finite():
+    torch = torch_cuda()
+    c = Cache([4], 16, 1, 64, 1, fill=0)
+    k = torch.ones(4, 64, device="cuda").bfloat16()
+    k[0, 3], k[1, 40], k[2, 63] = math.nan, math.inf, -math.inf
+    S.surge_op_cache_write(c.desc, 4, None, k, 64, k, 64)
+    out = [torch.empty_like(k) for _ in range(2)]
+    S.surge_op_cache_read(c.desc, 4, None, out[0], 64, out[1], 64)
+    for o in out:
+        nan = o.isnan()
+        assert nan[0, :32].all() and nan[1, 32:].all() and nan[2, 32:].all() and int(nan.sum()) == 96
+        assert (o[~nan] == 1).all()
+
+
+def test_entries_that_are_no_pages():
+    """Not written; read as NaN; lengths out of range are clamped."""
+    torch = torch_cuda()
+    c = Cache([40, 40, 40], 16, 1, 32, 1, fill=0xAB)
+    good = c.table_np.copy()
+    c.table_np[0, 1], c.table_np[1, 0], c.table_np[2, 2] = -1, c.n_pages, 1 << 30
+    c.table.copy_(dev(c.table_np))
+    k = randn(gen(1), 120, 32).bfloat16()
+    want = c.pages.clone()
+    seq, pos = places([40] * 3, [40] * 3)
+    on = (c.table_np == good)[seq, pos // 16]
+    on_t = torch.from_numpy(on).cuda()
+    c.put(seq[on], pos[on], k[on_t], k[on_t], want)
+    S.surge_op_cache_write(c.desc, 120, None, k, 32, k, 32)
+    assert torch.equal(c.pages, want)
+    out = [torch.empty_like(k) for _ in range(2)]
+    S.surge_op_cache_read(c.desc, 120, None, out[0], 32, out[1], 32)
+    assert torch.equal(out[0][on_t].double(), values(*quantized(k[on_t]))) and out[0][~on_t].isnan().all()
+    c.lengths.copy_(dev([-5, 1 << 30, 0]))
+    S.surge_op_cache_write(c.desc, 120, None, torch.zeros_like(k), 32, k, 32)
+    seq, pos = places([0, 40, 0], [40] * 3)
+    on = (pos >= 0) & (c.table_np == good)[seq, np.maximum(pos, 0) // 16]
+    c.put(seq[on], pos[on], torch.zeros_like(k)[:on.sum()], k[torch.from_numpy(on).cuda()], want)
+    assert torch.equal(c.pages, want)
+
+
+# ---------------------------------------------------------------------------
+# Attention
+# ---------------------------------------------------------------------------
+
+def attend(c, q, rows, heads, causal, out, workspace=None, stream=None, cu=None, max_rows=None):
+    torch = torch_cuda()
+    max_rows = max(max(rows), 1) if max_rows is None else max_rows
+    need = S.surge_cache_attention_workspace(c.desc, max_rows, heads)
+    if workspace is None and need:
+        workspace = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    S.surge_op_cache_attention(c.desc, sum(rows), cu_of(rows) if cu is None else cu, max_rows, heads,
+                               causal, c.dh ** -0.5, q, q.stride(0), workspace, out, out.stride(0),
+                               stream or torch.cuda.current_stream())
+    return need
+
+
+def reference(c, q, rows, heads, causal):
+    """Output and tolerance.  A probability is off by its rounding to bf16 and
+    by its score's fp32 error (dh + 2 roundings of the sum of magnitudes, as a
+    relative error, plus 8 roundings around the exponential); the sums add a
+    rounding per 32-key step and part."""
+    torch = torch_cuda()
+    hk, dh = c.hk, c.dh
+    G = heads // hk
+    ref = torch.zeros(sum(rows), heads * dh, dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(ref)
+    at = 0
+    for i, r in enumerate(rows):
+        n = int(c.lengths_np[i])
+        if r and n:
+            k, v = (x.permute(1, 0, 2).contiguous() for x in c.held[i])
+            x = q[at:at + r].double().view(r, hk, G, dh).permute(1, 0, 2, 3).reshape(hk, r * G, dh)
+            kt = k.transpose(1, 2).contiguous()
+            s = torch.bmm(x, kt) * dh ** -0.5
+            pos = torch.arange(n - r, n, device="cuda").repeat_interleave(G)
+            hidden = torch.arange(n, device="cuda") > pos[:, None] if causal else \
+                torch.zeros(r * G, n, dtype=torch.bool, device="cuda")
+            s = torch.where(hidden, -math.inf, s)
+            none = hidden.all(1)
+            s[:, none] = 0.0
+            p = torch.softmax(s, 2)
+            p[:, none] = 0.0
+            o, o_abs = torch.bmm(p, v), torch.bmm(p, v.abs())
+            size = torch.where(hidden, 0.0, torch.bmm(x.abs(), kt.abs())).amax(2, keepdim=True) * dh ** -0.5
+            rel = BF16 + 2 * (dh + 2) * F32 * size + (16 + 2 * (n // 32 + 1)) * F32
+            t = BF16 * o.abs() + 1.01 * rel * o_abs
+            for y, to in ((o, ref), (t, tol)):
+                to[at:at + r] = y.view(hk, r, G, dh).permute(1, 0, 2, 3).reshape(r, -1)
+        at += r
+    return ref, tol
+
+
+MIX = [(40, 5), (33, 3), (70, 2), (1, 1), (31, 31), (32, 0), (33, 32), (0, 4), (64, 1), (65, 64), (127, 65),
+       (128, 7), (2, 9), (500, 1), (3, 1), (257, 129), (1000, 16), (16, 17), (15, 1), (1500, 40)]
+
+
+def check(c, rows, heads, causal, seed, pad=8):
+    torch = torch_cuda()
+    n, w = sum(rows), heads * c.dh
+    q, _ = strided(randn(gen(seed), n, w).bfloat16(), pad)
+    out = torch.full((n + 2, w + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    need = attend(c, q, rows, heads, causal, out)
+    ref, tol = reference(c, q, rows, heads, causal)
+    within(out[:n, :w], ref, tol)
+    assert (out[n:] == 7).all() and (out[:, w:] == 7).all()
+    return need, out
+
+
+HEADS = [(16, 1, 1, 32), (32, 12, 12, 64), (16, 6, 2, 32), (64, 8, 1, 128), (128, 9, 3, 64), (256, 4, 2, 128),
+         (32, 16, 4, 128), (64, 40, 1, 64), (16, 5, 5, 128), (16, 32, 8, 32)]
+
+
+@pytest.mark.parametrize("page,heads,hk,dh", HEADS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention(page, heads, hk, dh, causal):
+    """All together: the lengths and row counts of MIX, unwritten places NaN."""
+    c = Cache([n for n, _ in MIX], page, hk, dh, heads, room=9).fill(page)
+    check(c, [r for _, r in MIX], heads, causal, dh)
+
+
+@pytest.mark.parametrize("page,heads,hk,dh", HEADS)
+@pytest.mark.parametrize("rows", [1, 2, 3, 5, 9, 20])
+def test_attention_of_steps(page, heads, hk, dh, rows):
+    """A few rows for each of several sequences, without offsets."""
+    torch = torch_cuda()
+    lengths = [1, 90, 0, 17, 64, 33, 500, 2, 130]
+    c = Cache(lengths, page, hk, dh, heads + rows).fill(page + 1)
+    for causal in (True, False):
+        q = randn(gen(rows), rows * len(lengths), heads * dh).bfloat16()
+        out = torch.full_like(q, math.nan)
+        need = S.surge_cache_attention_workspace(c.desc, rows, heads)
+        ws = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+        S.surge_op_cache_attention(c.desc, len(q), None, rows, heads, causal, dh ** -0.5, q, heads * dh,
+                                   ws, out, heads * dh, torch.cuda.current_stream())
+        within(out, *reference(c, q, [rows] * len(lengths), heads, causal))
+
+
+# Keys split over units: ends inside a block and a page, parts of one key.
+LONG = [([5000], [1], 64, 4, 4, 64), ([20_011], [1], 16, 32, 8, 128), ([8193, 5], [3, 5], 32, 2, 2, 32),
+        ([3001], [40], 64, 2, 1, 64), ([70_001], [1], 128, 1, 1, 128), ([2049, 100], [200, 3], 32, 2, 2, 128),
+        ([4097], [150], 16, 8, 2, 64), ([257], [1], 256, 1, 1, 64), ([9000, 3, 0, 40_000, 777], [2, 1, 1, 5, 4], 32, 8, 2, 128),
+        ([6000], [700], 64, 4, 1, 128), ([4100, 1030], [33, 5], 64, 8, 1, 128), ([2600], [9], 64, 16, 2, 128)]
+
+
+@pytest.mark.parametrize("lengths,rows,page,heads,hk,dh", LONG)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_over_long_sequences(lengths, rows, page, heads, hk, dh, causal):
+    torch = torch_cuda()
+    c = Cache(lengths, page, hk, dh, sum(lengths)).fill(1)
+    _, out = check(c, rows, heads, causal, 2)
+    again = check(c, rows, heads, causal, 2)[1]
+    assert torch.equal(out, again)  # no order of arrival in the result
+
+
+def test_attention_of_prompts_without_a_cache_before():
+    """Rows for every position of sequences, one tile and more."""
+    lengths = [130, 64, 1, 257, 640]
+    c = Cache(lengths, 16, 2, 64, 1).fill(3)
+    check(c, lengths, 4, True, 4)
+
+
+def test_attention_leaves_rows_beyond_max_rows():
+    torch = torch_cuda()
+    c = Cache([50, 40], 16, 2, 64, 1).fill(3)
+    q = randn(gen(1), 12, 128).bfloat16()
+    full, out = (torch.full((12, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    attend(c, q, [9, 3], 2, True, full)
+    attend(c, q, [9, 3], 2, True, out, max_rows=4)  # 4 rows of 2 heads' groups are in one tile of 16
+    assert torch.equal(out[:4], full[:4]) and torch.equal(out[9:], full[9:])
+    assert (out[4:9] == 7).all()
+
+
+SHAPES = [([50], [1], 4, 2, 64), ([130, 40], [3, 1], 2, 2, 32), ([77], [9], 8, 2, 128), ([300], [50], 2, 2, 64),
+          ([90], [33], 2, 1, 128), ([300], [70], 4, 4, 32), ([9000], [1], 4, 2, 64), ([20_011], [1], 32, 8, 128),
+          ([3001], [40], 2, 2, 64), ([2049], [200], 2, 2, 128)]
+
+
+def agrees(got, ref, tol):
+    torch = torch_cuda()
+    bad = ref.isnan()
+    assert torch.equal(got.isnan(), bad), (int(got.isnan().sum()), int(bad.sum()))
+    if not bad.all():
+        within(got[~bad], ref[~bad], tol[~bad])
+
+
+@pytest.mark.parametrize("lengths,rows,heads,hk,dh", SHAPES)
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_attention_of_marked_keys(lengths, rows, heads, hk, dh, which):
+    """A key or value marked NaN at the last position of a sequence, in one key
+    head: the last row of that head's group is NaN, and none before it."""
+    torch = torch_cuda()
+    c = Cache(lengths, 16, hk, dh, 1).fill(5)
+    q = randn(gen(6), sum(rows), heads * dh).bfloat16()
+    ref, tol = reference(c, q, rows, heads, True)
+    n, G = lengths[0], heads // hk
+    f = c.fields()
+    f["kv".index(which) + 2][c.table_np[0, (n - 1) // 16], hk - 1, (n - 1) % 16, dh // 32 - 1] = 255
+    ref[rows[0] - 1, (hk - 1) * G * dh:] = math.nan
+    out = torch.full_like(q, 7.0)
+    attend(c, q, rows, heads, True, out)
+    agrees(out, ref, tol)
+    attend(c, q, rows, heads, False, out)
+    nan = out.isnan()
+    assert nan[:rows[0], (hk - 1) * G * dh:].all() and int(nan.sum()) == rows[0] * G * dh
+
+
+@pytest.mark.parametrize("lengths,rows,heads,hk,dh", SHAPES)
+def test_attention_of_missing_pages_and_nan_queries(lengths, rows, heads, hk, dh):
+    torch = torch_cuda()
+    c = Cache(lengths, 16, hk, dh, 1).fill(5)
+    q = randn(gen(6), sum(rows), heads * dh).bfloat16()
+    out = torch.full_like(q, 7.0)
+    ref, tol = reference(c, q, rows, heads, True)
+    q[0, 5] = math.nan
+    ref[0, :dh] = math.nan
+    attend(c, q, rows, heads, True, out)
+    agrees(out, ref, tol)
+    entry = (lengths[0] - 1) // 16
+    c.table[0, entry] = c.n_pages
+    first = lengths[0] - rows[0]
+    sees = [j for j in range(rows[0]) if first + j >= entry * 16]
+    ref[sees] = math.nan
+    attend(c, q, rows, heads, True, out)
+    agrees(out, ref, tol)
+
+
+@pytest.mark.parametrize("lengths,rows,heads,hk,dh", SHAPES)
+def test_attention_of_scores_past_the_largest_float(lengths, rows, heads, hk, dh):
+    """A row whose scores are all -inf, and one whose largest is +inf: NaN."""
+    torch = torch_cuda()
+    c = Cache(lengths, 16, hk, dh, 1)
+    for i, n in enumerate(lengths):
+        k = torch.full((n, hk * dh), 2.0 ** 120, device="cuda").bfloat16()
+        c.put(i, np.arange(n), k, torch.ones_like(k))
+    for sign in (1, -1):
+        q = torch.full((sum(rows), heads * dh), sign * 2.0 ** 100, device="cuda").bfloat16()
+        q[-1] = 0
+        out = torch.full_like(q, 7.0)
+        attend(c, q, rows, heads, True, out)
+        assert out[:-1].isnan().all()
+        assert (out[-1] == 1).all()  # every score 0: the mean of the values
+
+
+@pytest.mark.parametrize("up", [True, False])
+def test_attention_of_scores_that_rise_and_fall(up):
+    """Scores that grow or fall by hundreds along the keys: the running maximum
+    moves in every block, or all but the first keys vanish."""
+    torch = torch_cuda()
+    n, dh = 3000, 64
+    c = Cache([n], 32, 1, dh, 1)
+    ramp = torch.linspace(-400 if up else 400, 400 if up else -400, n, device="cuda")
+    k = torch.zeros(n, dh, device="cuda")
+    k[:, 0] = ramp
+    v = randn(gen(1), n, dh).bfloat16()
+    c.put(0, np.arange(n), k.bfloat16(), v)
+    c.held = [[values(*quantized(x)).view(n, 1, dh) for x in (k.bfloat16(), v)]]
+    q = torch.zeros(20, dh, device="cuda")
+    q[:, 0] = torch.linspace(0.1, 30, 20, device="cuda")
+    q = q.bfloat16()
+    out = torch.empty_like(q)
+    attend(c, q, [20], 1, True, out)
+    within(out, *reference(c, q, [20], 1, True))
+
+
+def test_pages_past_32_bits():
+    """Pages whose addresses pass 2^32 bytes."""
+    torch = torch_cuda()
+    page, hk, dh = 256, 8, 128
+    size = S.surge_cache_page_bytes(page, hk, dh)
+    n_pages = (1 << 32) // size + 40
+    pages = torch.full((n_pages, size), 255, dtype=torch.uint8, device="cuda")
+    c = Cache([700, 300], page, hk, dh, 1)
+    far = n_pages - 1 - np.arange(5)
+    c.table_np[0, :3], c.table_np[1, :2] = far[:3], [0, far[4]]
+    c.pages, c.n_pages = pages, n_pages
+    c.table = dev(c.table_np)
+    c.desc = S.KVCache(pages, n_pages, page, hk, dh, c.table, c.width, 2, c.lengths, 700)
+    g = gen(1)
+    k, v = (randn(g, 1000, hk * dh).bfloat16() for _ in range(2))
+    cu = dev([0, 700, 1000])
+    S.surge_op_cache_write(c.desc, 1000, cu, k, hk * dh, v, hk * dh)
+    out = [torch.empty_like(k) for _ in range(2)]
+    S.surge_op_cache_read(c.desc, 1000, cu, out[0], hk * dh, out[1], hk * dh)
+    assert torch.equal(out[0].double(), values(*quantized(k)))
+    assert torch.equal(out[1].double(), values(*quantized(v)))
+    held = [values(*quantized(x)).view(1000, hk, dh) for x in (k, v)]
+    c.held = [[x[:700] for x in held], [x[700:] for x in held]]
+    for rows in ([2, 1], [100, 80]):
+        check(c, rows, 16, True, 3)
+
+
+def test_refused_workspaces():
+    torch = torch_cuda()
+    c = Cache([9000], 64, 2, 64, 1).fill(1)
+    q = randn(gen(1), 1, 128).bfloat16()
+    out = torch.full_like(q, 7.0)
+    need = S.surge_cache_attention_workspace(c.desc, 1, 2)
+    assert need > 0
+    ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+    for bad in (None, ws[:need - 1], ws[8:]):
+        with pytest.raises(S.SurgeError) as e:
+            S.surge_op_cache_attention(c.desc, 1, None, 1, 2, True, 0.125, q, 128, bad, out, 128)
+        assert e.value.status in (S.SURGE_ERR_INVALID_ARGUMENT, S.SURGE_ERR_CAPACITY)
+    torch.cuda.synchronize()
+    assert (out == 7).all()
+
+
+def test_attention_on_two_streams():
+    """One cache, two streams, a workspace each."""
+    torch = torch_cuda()
+    c = Cache([9000, 12_000], 64, 2, 128, 5).fill(1)
+    q = [randn(gen(i), 3, 1024).bfloat16() for i in (1, 2)]
+    want = [torch.empty_like(x) for x in q]
+    for x, o in zip(q, want):
+        need = attend(c, x, [1, 2], 8, True, o)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [torch.empty_like(o) for o in want]
+    spaces = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cu = cu_of([1, 2])
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, o, s, w in zip(q, got, streams, spaces):
+            attend(c, x, [1, 2], 8, True, o, w, s, cu)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# ---------------------------------------------------------------------------
+# Drafts
+# ---------------------------------------------------------------------------
+
+def verified(p, q, drafts, counts, u):
+    """Tokens and counts by the definition, in 64 bits on the host."""
+    p = p.double().cpu().numpy()
+    q = None if q is None else q.double().cpu().numpy()
+    x, u = drafts.cpu().numpy(), u.double().cpu().numpy()
+    n, k1, vocab = p.shape
+    tokens, accepted = np.full((n, k1), -1, np.int32), np.zeros(n, np.int32)
+    for i in range(n):
+        c = min(max(int(counts[i]), 0), k1 - 1)
+        a = 0
+        while a < c and 0 <= x[i, a] < vocab and \
+                u[i, a] * (1.0 if q is None else q[i, a, x[i, a]]) < p[i, a, x[i, a]]:
+            tokens[i, a] = x[i, a]
+            a += 1
+        accepted[i] = a
+        target = np.where(p[i, a] > 0, p[i, a], 0.0)
+        r = target
+        if a < c:
+            if q is not None:
+                with np.errstate(invalid="ignore"):
+                    d = p[i, a] - q[i, a]
+                r = np.where(d > 0, d, 0.0)
+            elif 0 <= x[i, a] < vocab:
+                r = target.copy()
+                r[x[i, a]] = 0
+            if not r.sum() > 0:
+                r = target
+        total = r.sum()
+        if total > 0 and np.isfinite(total):
+            over = np.flatnonzero((np.cumsum(r) > u[i, -1] * total) & (r > 0))
+            tokens[i, a] = over[0] if len(over) else np.flatnonzero(r > 0)[-1]
+    return tokens, accepted
+
+
+def verify(p, q, drafts, counts, u, n_drafts="given", pad=0, stream=None):
+    torch = torch_cuda()
+    n, k1, vocab = p.shape
+    if pad:
+        p = torch.nn.functional.pad(p, (0, pad), value=1e30)
+        q = None if q is None else torch.nn.functional.pad(q, (0, pad), value=-1e30)
+    tokens = torch.full((n, k1), 77, dtype=torch.int32, device="cuda")
+    accepted = torch.full((n,), 77, dtype=torch.int32, device="cuda")
+    need = S.surge_verify_workspace(n, vocab)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None
+    S.surge_op_verify_drafts(n, k1 - 1, vocab, None if n_drafts is None else dev(counts), drafts, p,
+                             vocab + pad, q, vocab + pad, u, ws, tokens, accepted,
+                             stream or torch.cuda.current_stream())
+    return tokens.cpu().numpy(), accepted.cpu().numpy()
+
+
+def draft_inputs(n, k, vocab, seed, sharp=3.0, near=1.0):
+    torch = torch_cuda()
+    g = gen(seed)
+    logits = sharp * randn(g, n, k + 1, vocab)
+    p = torch.softmax(logits, 2)
+    q = torch.softmax(logits[:, :k] + near * randn(g, n, k, vocab), 2)
+    noise = torch.rand(n, k, vocab, generator=g, device="cuda").clamp_min(1e-30)
+    drafts = (q / -torch.log(noise)).argmax(2).int() if k else torch.zeros(n, 0, dtype=torch.int32, device="cuda")
+    return p, q, drafts, torch.rand(n, k + 1, generator=g, device="cuda")
+
+
+VERIFY = [(1, 1, 1), (3, 2, 2), (5, 4, 63), (40, 3, 100), (9, 7, 1000), (2, 4, 4095), (2, 4, 4096), (3, 4, 4097),
+          (64, 4, 30_522), (1, 4, 30_522), (300, 1, 257), (5, 70, 500), (4, 6, 100_003), (1, 2, 262_145),
+          (600, 2, 5000), (3, 0, 777), (2, 130, 64), (1, 1, 1 << 22)]
+
+
+@pytest.mark.parametrize("n,k,vocab", VERIFY)
+@pytest.mark.parametrize("probs", [True, False])
+def test_verify_drafts(n, k, vocab, probs):
+    p, q, drafts, u = draft_inputs(n, k, vocab, n + k + vocab)
+    if not k:
+        probs = False
+    counts = np.random.default_rng(n).integers(-1, k + 2, n)
+    counts[0] = k
+    for c, given in ((counts, "given"), (np.full(n, k), None)):
+        want = verified(p, q if probs else None, drafts, c, u)
+        got = verify(p, q if probs else None, drafts, c, u, given, pad=5 if n % 2 else 0)
+        assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+
+
+def test_verify_draws_from_the_target():
+    """Drafts drawn from q and u even: the first token has the target's
+    distribution (mean of 40,000 draws, five standard deviations)."""
+    torch = torch_cuda()
+    n, vocab = 40_000, 12
+    p, q, _, _ = draft_inputs(1, 1, vocab, 3, sharp=1.0, near=1.5)
+    g = gen(9)
+    drafts = torch.multinomial(q[0, 0].expand(n, vocab), 1, generator=g).int()
+    u = torch.rand(n, 2, generator=g, device="cuda")
+    tokens, _ = verify(p.expand(n, 2, vocab).contiguous(), q.expand(n, 1, vocab).contiguous(), drafts,
+                       np.ones(n), u)
+    share = np.bincount(tokens[:, 0], minlength=vocab) / n
+    want = p[0, 0].double().cpu().numpy()
+    assert (np.abs(share - want) <= 5 * np.sqrt(want * (1 - want) / n) + 1e-9).all()
+
+
+def test_verify_at_the_edges():
+    """Drafts outside the vocabulary, rows that are not finite or nothing, q that
+    leaves nothing over, u at 0, next to 1 and beyond."""
+    torch = torch_cuda()
+    n, k, vocab = 14, 2, 5000
+    p, q, drafts, u = draft_inputs(n, k, vocab, 1)
+    drafts[0, 0], drafts[1, 0], drafts[2, 1] = -1, vocab, 1 << 30
+    p[3] = 0                       # nothing to draw: -1
+    p[4, 0, 7] = math.inf          # infinite: -1
+    drafts[4, 0] = 3
+    u[4, 0] = 0.999999
+    p[5, :, ::2] = math.nan        # counts as 0
+    p[6, 0] = q[6, 0]              # rejected by u beyond 1, nothing left over: the target's own
+    u[6, 0] = 2.0
+    u[7] = 0.0
+    u[8] = 1 - 2.0 ** -24
+    u[9, k] = 1.0                  # beyond every sum: the last token that weighs anything
+    p[9, :, vocab - 900:] = 0
+    u[10] = math.nan
+    q[11] = math.nan
+    p[12, :, :4500] = 0            # the first tokens weigh nothing, u 0
+    u[12, k] = 0.0
+    p[13] = -p[13]
+    counts = np.full(n, k)
+    for x in (q, None):
+        want = verified(p, x, drafts, counts, u)
+        got = verify(p, x, drafts, counts, u)
+        assert np.array_equal(got[0], want[0]), (got[0], want[0])
+        assert np.array_equal(got[1], want[1])
+    assert got[0][3, 0] == -1 and got[0][13, 0] == -1
+
+
+def test_verify_takes_the_token_on_either_side_of_a_border():
+    """Sums that are exact: u at a border takes the next token."""
+    torch = torch_cuda()
+    vocab = 1 << 14
+    u = torch.tensor([[0.0], [0.25], [0.5], [0.5 - 2.0 ** -25], [1 - 2.0 ** -24], [3 * 2.0 ** -14]], device="cuda")
+    p = torch.full((len(u), 1, vocab), 1.0 / vocab, device="cuda")
+    none = torch.zeros(len(u), 0, dtype=torch.int32, device="cuda")
+    got, _ = verify(p, None, none, np.zeros(len(u)), u)
+    assert got[:, 0].tolist() == [0, vocab // 4, vocab // 2, vocab // 2 - 1, vocab - 1, 3]
+
+
+# ---------------------------------------------------------------------------
+# The operators together: a step of a decoder
+# ---------------------------------------------------------------------------
+
+class Decoder:
+    """Steps of a batch of answers: the drafts' and the last token's keys and
+    values go into the cache, their queries attend, the logits of the attended
+    rows are the target's, the drafts are checked, and the lengths go back to
+    what was accepted."""
+
+    def __init__(self, lengths, drafts, page, heads, hk, dh, vocab, seed):
+        torch = torch_cuda()
+        self.n, self.k, self.heads, self.vocab = len(lengths), drafts, heads, vocab
+        rows = self.n * (drafts + 1)
+        self.c = c = Cache(lengths, page, hk, dh, seed, room=64).fill(seed)
+        g = gen(seed)
+        self.head = randn(g, heads * dh, vocab) / math.sqrt(heads * dh)
+        self.x = randn(g, rows, (heads + 2 * hk) * dh).bfloat16()  # Q | K | V of the step's rows
+        self.q_probs = torch.softmax(randn(g, self.n, drafts, vocab), 2)
+        self.drafts = torch.randint(0, vocab, (self.n, drafts), generator=g, device="cuda", dtype=torch.int32)
+        self.u = torch.rand(self.n, drafts + 1, generator=g, device="cuda")
+        self.out = torch.empty(rows, heads * dh, dtype=torch.bfloat16, device="cuda")
+        self.p = torch.empty(self.n, drafts + 1, vocab, device="cuda")
+        self.tokens = torch.empty(self.n, drafts + 1, dtype=torch.int32, device="cuda")
+        self.accepted = torch.empty(self.n, dtype=torch.int32, device="cuda")
+        self.ws = torch.empty(max(16, S.surge_cache_attention_workspace(c.desc, drafts + 1, heads)),
+                              dtype=torch.uint8, device="cuda")
+        self.vws = torch.empty(max(16, S.surge_verify_workspace(self.n, vocab)), dtype=torch.uint8, device="cuda")
+
+    def step(self, stream):
+        torch = torch_cuda()
+        c, m = self.c, self.k + 1
+        rows, ld, qd = self.n * m, self.x.shape[1], self.heads * self.c.dh
+        kd = c.hk * c.dh
+        c.lengths.add_(m)
+        S.surge_op_cache_write(c.desc, rows, None, self.x[:, qd:], ld, self.x[:, qd + kd:], ld, stream)
+        S.surge_op_cache_attention(c.desc, rows, None, m, self.heads, True, c.dh ** -0.5, self.x, ld, self.ws,
+                                   self.out, qd, stream)
+        torch.softmax((self.out.float() @ self.head).view(self.n, m, -1), 2, out=self.p)
+        S.surge_op_verify_drafts(self.n, self.k, self.vocab, None, self.drafts, self.p, self.vocab,
+                                 self.q_probs, self.vocab, self.u, self.vws, self.tokens, self.accepted, stream)
+        c.lengths.sub_(self.k - self.accepted)
+
+
+def test_decoder_steps():
+    """Each step against the definitions, positions overwritten after rejections."""
+    torch = torch_cuda()
+    d = Decoder([90, 1, 33, 0, 700, 3000], 3, 16, 8, 2, 64, 500, 1)
+    c, g = d.c, gen(2)
+    for _ in range(5):
+        d.x.copy_(randn(g, *d.x.shape))
+        d.u.copy_(torch.rand(d.u.shape, generator=g, device="cuda"))
+        before = c.lengths.cpu().numpy().astype(np.int64)
+        d.step(torch.cuda.current_stream())
+        qd, kd, m = d.heads * c.dh, c.hk * c.dh, d.k + 1
+        for i in range(d.n):
+            for w in range(2):
+                new = d.x[i * m:(i + 1) * m, qd + w * kd:qd + (w + 1) * kd]
+                c.held[i][w] = torch.cat([c.held[i][w][:before[i]], values(*quantized(new)).view(m, c.hk, c.dh)])
+        c.lengths_np = before + m
+        within(d.out, *reference(c, d.x[:, :qd], [m] * d.n, d.heads, True))
+        want = verified(d.p, d.q_probs, d.drafts, np.full(d.n, d.k), d.u)
+        assert np.array_equal(d.tokens.cpu().numpy(), want[0]) and np.array_equal(d.accepted.cpu().numpy(), want[1])
+        assert np.array_equal(c.lengths.cpu().numpy(), before + 1 + want[1])
+
+
+def test_decoder_steps_captured_and_replayed():
+    """Two decoders in a graph each, replayed as their answers grow, with new
+    inputs, eager work and synchronisations between: the eager step's bits."""
+    torch = torch_cuda()
+    make = [lambda: Decoder([90, 1, 33, 0, 700, 5000], 3, 16, 8, 2, 64, 500, 1),
+            lambda: Decoder([2000] * 3, 0, 32, 32, 8, 128, 3001, 2)]
+    eager, replayed = [f() for f in make], [f() for f in make]
+    stream = torch.cuda.Stream()
+    graphs = []
+    for d in replayed:
+        start = d.c.lengths.clone()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):  # once before, for what torch's own product sets up
+            d.step(stream)
+        torch.cuda.synchronize()
+        d.c.lengths.copy_(start)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            d.step(torch.cuda.current_stream())
+        graphs.append(graph)
+    g = gen(3)
+    for step in range(6):
+        for d, r in zip(eager, replayed):
+            d.x.copy_(randn(g, *d.x.shape))
+            d.u.copy_(torch.rand(d.u.shape, generator=g, device="cuda"))
+            r.x.copy_(d.x)
+            r.u.copy_(d.u)
+        for d, r, graph in zip(eager, replayed, graphs):
+            graph.replay()
+            if step % 2:
+                torch.cuda.synchronize()
+            d.step(torch.cuda.current_stream())
+        for d, r in zip(eager, replayed):
+            assert torch.equal(d.out, r.out) and torch.equal(d.tokens, r.tokens)
+            assert torch.equal(d.accepted, r.accepted) and torch.equal(d.c.lengths, r.c.lengths)
+    for r, graph in zip(replayed, graphs):  # both at the same time, on a stream each
+        r.start = r.c.lengths.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        r.want = r.out.clone()
+        r.c.lengths.copy_(r.start)
+    streams = [torch.cuda.Stream() for _ in replayed]
+    torch.cuda.synchronize()
+    for graph, s in zip(graphs, streams):
+        with torch.cuda.stream(s):
+            graph.replay()
+    torch.cuda.synchronize()
+    for r in replayed:
+        assert torch.equal(r.out, r.want)
