@@ -69,7 +69,9 @@ struct VerifyDrafts {
   int64_t ld_p, ld_q;
   const float* u;
   int32_t *tokens, *accepted;
+  double* sums;  // workspace of verify_workspace bytes
 };
+int64_t verify_workspace(int64_t n_seqs, int vocab);
 hipError_t launch_verify_drafts(int64_t n_seqs, const VerifyDrafts& a, hipStream_t stream);
 
 }  // namespace surge

@@ -234,6 +234,7 @@ surge_status surge_verify_workspace(int64_t n_seqs, int32_t vocab, int64_t* byte
   *bytes = 0;
   if (n_seqs < 0 || n_seqs > kMaxSeqs || vocab < 1 || vocab > kMaxVocab)
     return fail(SURGE_ERR_INVALID_ARGUMENT, "n_seqs=%lld, vocab=%d", (long long)n_seqs, vocab);
+  *bytes = verify_workspace(n_seqs, vocab);
   return SURGE_OK;
 }
 
@@ -269,10 +270,20 @@ surge_status surge_op_verify_drafts(int64_t n_seqs, int32_t max_drafts, int32_t 
   if (ld_p < vocab || ld_p > kMostLength || (d_q && (ld_q < vocab || ld_q > kMostLength)))
     return fail(SURGE_ERR_INVALID_ARGUMENT, "row strides %lld and %lld of p and q, vocab=%d",
                 (long long)ld_p, (long long)ld_q, vocab);
+  const int64_t need = verify_workspace(n_seqs, vocab);
+  if (need > 0) {
+    CHECK(check_vector("workspace", d_workspace, true));
+    if (workspace_bytes < need)
+      return fail(SURGE_ERR_CAPACITY, "workspace of %lld bytes, %lld are needed",
+                  (long long)workspace_bytes, (long long)need);
+  }
+  // A launch's threads: 1024 for every 32,768 tokens of a sequence.
+  if (n_seqs * ((vocab + 32767) / 32768) > kMostThreads / 1024)
+    return fail(SURGE_ERR_CAPACITY, "too many sequences and tokens for one call");
   int dev = 0, n_cus = 0;
   CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
-  const VerifyDrafts a = {max_drafts, vocab, d_n_drafts, d_drafts, d_p, d_q, ld_p, ld_q,
-                          d_u,        d_tokens, d_accepted};
+  const VerifyDrafts a = {max_drafts, vocab, d_n_drafts, d_drafts,   d_p, d_q,
+                          ld_p,       ld_q,  d_u,        d_tokens,   d_accepted, (double*)d_workspace};
   HIP_TRY(launch_verify_drafts(n_seqs, a, (hipStream_t)hip_stream));
   return SURGE_OK;
 }
