@@ -338,6 +338,227 @@ __global__ __launch_bounds__(256) void few_rows_kernel(CacheAttention a) {
   }
 }
 
+// Many rows: four waves of 32 share blocks of 64 keys in LDS, decoded to bf16 by
+// all of them, each wave a tile of 16 keys.  A block's codes are loaded two blocks
+// ahead and decoded one ahead.
+//
+// Chunk c of row r is stored at c ^ f(r), so that neither the reads of K (a chunk
+// of 32 rows), the transposing reads of V (64 bytes of four consecutive rows) nor,
+// at d_head 128, the writes (a chunk of 16 rows) have bank conflicts.
+template <int CPR>
+__device__ __forceinline__ uint32_t kv_position(int row, int chunk) {
+  if constexpr (CPR == 16) return row * 16 + (chunk ^ ((row & 3) << 2 | (row >> 2 & 3)));
+  if constexpr (CPR == 8) return row * 8 + (chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3)));
+  return swz<4>(row, chunk);
+}
+
+__device__ __forceinline__ float over_halves(float v, float (*op)(float, float)) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int DH>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(CacheAttention a) {
+  using L = PageLayout<DH>;
+  constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8, STEPS = DH / 32, KB = 64, T = KB / 32;
+  constexpr uint32_t ROW = DH * 2, BUF = KB * ROW;
+  __shared__ __attribute__((aligned(256))) u32x4 sKV[4 * BUF / 16];  // K blocks by parity, then V blocks
+  Unit u;
+  if (!unit_of(a, blockIdx.x, &u)) return;
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.group;
+  const int row0 = u.row0 + wave * 32;
+  const bool active = row0 < u.rows;  // a wave without rows still decodes
+  const int row = min(row0 + col, u.rows - 1);
+  const int limit = min(row_limit(a, u, row), u.k1);
+  const int least = min(row_limit(a, u, min(row0, u.rows - 1)), u.k1);            // that every row sees
+  const int most_keys = min(row_limit(a, u, min(row0 + 31, u.rows - 1)), u.k1);   // that some row sees
+
+  bf16x8 qf[KSTEPS];
+  const uint16_t* q = a.q + (int64_t)(u.q_beg + row / G) * a.ld_q + (u.kvh * G + row % G) * DH;
+#pragma unroll
+  for (int kk = 0; kk < KSTEPS; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(q + (kk * 2 + half) * 8);
+
+  const int64_t head_at = u.kvh * L::head_bytes(a.c.page_shift);
+  const int shift = a.c.page_shift, mask = (1 << shift) - 1;
+  const int n = (max(u.k1 - u.k0, 0) + KB - 1) / KB;
+  // Pages of this wave's tile of blocks first .. first + 63.
+  auto pages_from = [&](int first) {
+    const int key = u.k0 + (first + lane) * KB + 16 * wave;
+    if (key >= u.k1) return 0;
+    const int page = a.c.table[u.seq * a.c.ld_table + (key >> shift)];
+    return page >= 0 && page < a.c.n_pages ? page : -1;
+  };
+  int pages = n > 0 ? pages_from(0) : 0;
+  Quarter<DH> raw_k, raw_v;
+  uint32_t raw_ks = 0, raw_vs = 0;
+  bool raw_bad = false;
+  auto load = [&](int i) {
+    if (i > 0 && (i & 63) == 0) pages = pages_from(i);
+    const int page = __builtin_amdgcn_readlane(pages, i & 63);
+    raw_bad = page < 0;
+    const uint8_t* p = a.c.pages + max(page, 0) * a.c.page_bytes + head_at;
+    const int slot = ((u.k0 + i * KB + 16 * wave) & mask) + (lane & 15), quarter = lane >> 4;
+    raw_k.load(p + L::codes(shift, slot, 0) + quarter * (DH / 8));
+    raw_v.load(p + L::codes(shift, slot, 1) + quarter * (DH / 8));
+    raw_ks = p[L::scales(shift, slot, 0) + quarter * L::SCALES / 4];
+    raw_vs = p[L::scales(shift, slot, 1) + quarter * L::SCALES / 4];
+  };
+  auto decode = [&](int i) {
+    float k_scale, v_scale;
+    const int r = 16 * wave + (lane & 15);
+    scales_of(raw_ks, raw_vs, u.k0 + i * KB + r < u.k1, raw_bad, &k_scale, &v_scale);
+    u32x4* const to = sKV + (i & 1) * (BUF / 16);
+#pragma unroll
+    for (int kk = 0; kk < STEPS; ++kk) {
+      const uint32_t at = kv_position<CPR>(r, (lane >> 4) * STEPS + kk);
+      to[at] = __builtin_bit_cast(u32x4, decode8(raw_k.w[kk], k_scale));
+      to[2 * (BUF / 16) + at] = __builtin_bit_cast(u32x4, decode8(raw_v.w[kk], v_scale));
+    }
+  };
+
+  const uint32_t lds = lds_address(sKV);
+  const int tr_key = 4 * half + ((lane & 15) >> 2);
+  const int tr_feat = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  uint32_t ka = lds + kv_position<CPR>(col, half) * 16u;
+  uint32_t va = lds + 2 * BUF + kv_position<CPR>(tr_key, tr_feat >> 3) * 16u + (tr_feat & 7) * 2u;
+  constexpr uint32_t H_SWZ = CPR == 4 ? 16 : 32;  // of 8 keys further on
+  auto k_fragment = [&](int t, int kk) {
+    return __builtin_bit_cast(
+        bf16x8, *(const __attribute__((address_space(3))) u32x4*)((ka ^ kk * 32) + t * 32 * ROW));
+  };
+  auto v_fragment = [&](int c, int dt) {
+    bf16x4 v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      v[h] = __builtin_bit_cast(
+          bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(
+                      (va ^ (dt * 64 ^ h * H_SWZ)) + (16 * c + 8 * h) * ROW)));
+    return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+
+  bool coarse = false;  // some row's maximum is 2^24 or more
+  float m_ref = -FLT_MAX, l_run = 0.0f;
+  f32x16 o[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
+
+  if (n > 0) {
+    load(0);
+    decode(0);
+    if (n > 1) load(1);
+  }
+  for (int i = 0; i < n; ++i) {
+    __syncthreads();  // the block is there, the other one read out
+    if (i + 1 < n) {
+      decode(i + 1);
+      if (i + 2 < n) load(i + 2);
+    }
+    const int key0 = u.k0 + i * KB;
+    if (active && key0 < most_keys) {
+      f32x16 s[T];
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < KSTEPS; ++kk)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
+      if (key0 + KB > least) {
+        const int seen = limit - key0 - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16 * T; ++r)
+          if (32 * (r >> 4) + 8 * (r >> 2 & 3) + (r & 3) >= seen) s[r >> 4][r & 15] = -INFINITY;
+      }
+      float most = s[0][0];
+#pragma unroll
+      for (int r = 1; r < 16 * T; ++r) most = fmaxf(most, s[r >> 4][r & 15]);
+      most = over_halves(most, max_of) * a.scale_log2;
+      if (__any(most > m_ref + 8.0f)) {
+        const float m_new = fmaxf(m_ref, most);
+        const float alpha = __builtin_amdgcn_exp2f(m_ref - m_new);
+        m_ref = m_new;
+        coarse = __any(fabsf(m_new) >= 0x1p24f);
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      }
+      // The reference is a rounded product, off from the exact ones of the
+      // exponentials by up to half of its step: where that is large, the products
+      // are rounded too.
+      float factor = a.scale_log2;
+      if (__builtin_expect(coarse, 0)) {
+#pragma unroll
+        for (int r = 0; r < 16 * T; ++r) s[r >> 4][r & 15] *= factor;
+        factor = 1.0f;
+      }
+#pragma unroll
+      for (int c = 0; c < 2 * T; ++c) {
+        bf16x8 pb;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[c >> 1][8 * (c & 1) + r], factor, -m_ref));
+          l_run += p;
+          pb[r] = (__bf16)p;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(c, dt), pb, o[dt], 0, 0, 0);
+      }
+    }
+    const uint32_t other = i & 1 ? 0u - BUF : BUF;
+    ka += other;
+    va += other;
+  }
+  l_run = over_halves(l_run, sum_of);
+  const bool seen = limit > u.k0;
+
+  // Register r of tile dt: feature dt 32 + 8 (r / 4) + 4 half + r % 4 of row col.
+  if (a.splits == 1 || u.limit <= a.chunk) {
+    __syncthreads();  // every wave has read its last block
+    if (!active) return;
+    const float inv = 1.0f / l_run;
+    u32x4* stage = sKV + wave * (32 * CPR);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint2 w;
+        w.x = seen ? pack_bf16x2(o[dt][4 * g] * inv, o[dt][4 * g + 1] * inv) : 0u;
+        w.y = seen ? pack_bf16x2(o[dt][4 * g + 2] * inv, o[dt][4 * g + 3] * inv) : 0u;
+        reinterpret_cast<uint2*>(stage + kv_position<CPR>(col, dt * 4 + g))[half] = w;
+      }
+    // Whole rows are stored, 16 bytes a lane.
+#pragma unroll
+    for (int j = 0; j < CPR / 2; ++j) {
+      const int r = j * (64 / CPR) + lane / CPR, chunk = lane % CPR;
+      const u32x4 w = stage[kv_position<CPR>(r, chunk)];
+      if (row0 + r < u.rows)
+        __builtin_nontemporal_store(
+            w, reinterpret_cast<u32x4*>(a.out + (int64_t)(u.q_beg + (row0 + r) / G) * a.ld_out +
+                                        (u.kvh * G + (row0 + r) % G) * DH + chunk * 8));
+    }
+    return;
+  }
+  if (row0 + col >= u.rows) return;
+  const int64_t slot = (int64_t)u.slot * a.tile_rows + wave * 32 + col;
+  if (half == 0) a.part_ml[slot] = make_float2(seen ? m_ref : -INFINITY, l_run);
+  float* po = a.part_o + slot * DH;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<float4*>(po + dt * 32 + g * 8 + half * 4) =
+          make_float4(o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]);
+}
+
 // Joins the parts of a row of one key head: a wave a row, in the order of the
 // keys.
 template <int DH>
@@ -384,6 +605,7 @@ hipError_t launch(const CacheAttention& a, hipStream_t stream) {
   if (a.tile_rows == 16) hipLaunchKernelGGL((few_rows_kernel<DH, 1>), grid, block, 0, stream, a);
   if (a.tile_rows == 32) hipLaunchKernelGGL((few_rows_kernel<DH, 2>), grid, block, 0, stream, a);
   if (a.tile_rows == 64) hipLaunchKernelGGL((few_rows_kernel<DH, 4>), grid, block, 0, stream, a);
+  if (a.tile_rows == 128) hipLaunchKernelGGL(tile_kernel<DH>, grid, block, 0, stream, a);
   if (a.splits > 1)
     hipLaunchKernelGGL(join_kernel<DH>, dim3((unsigned)(tiles * a.tile_rows / 4)), block, 0, stream, a);
   return hipGetLastError();
@@ -395,7 +617,7 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
                                  int64_t max_length, int n_cus) {
   CacheShape s;
   const int64_t rows = max_rows * group;
-  s.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  s.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   s.tiles = (rows + s.tile_rows - 1) / s.tile_rows;
   const int64_t units = n_seqs * n_kv_heads * s.tiles;
   const int64_t want = std::max<int64_t>(1, 4 * (int64_t)n_cus / units);
