@@ -46,17 +46,26 @@ struct CacheAttention {
   bool causal;
   float scale_log2;   // scale * log2(e)
   // Of cache_attention_shape.
-  int tile_rows, tiles, splits, chunk;
-  float2* part_ml;    // [sequence, tile, key head, split, row] (maximum in log2 units, sum)
-  float* part_o;      // [the same, d_head]
+  int tile_rows, block_keys, tiles, units, workers, least_share;
+  // Workspace, where there are workers: of the two slots that each has for the
+  // parts of its first and last unit, the rows' maxima (in log2 units) and sums,
+  // their outputs, and which workers have the parts of a unit.
+  float* part_o;     // [slot, row, d_head]
+  float2* part_ml;   // [slot, row]
+  int2* joins;       // [unit] first and last worker; first < 0: not cut
 };
 
 // How a call is cut into units: tiles of tile_rows rows (query * group + head
-// of the group) of each sequence, and their keys into at most `splits` ranges
-// of `chunk` keys.
+// of the group) of each (sequence, key head).  Their keys, in blocks of
+// block_keys, are shared out to `workers` workgroups, at least least_share blocks
+// each, or where that is 0 a unit is a workgroup's.
 struct CacheShape {
-  int tile_rows;
-  int64_t tiles, splits, chunk;
+  int tile_rows, block_keys, least_share;
+  int64_t tiles, units, workers;
+  int64_t slot_rows() const { return 2 * workers * tile_rows; }
+  int64_t workspace_bytes(int d_head) const {
+    return workers ? slot_rows() * (8 + 4 * (int64_t)d_head) + units * 8 : 0;
+  }
 };
 CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_heads, int group, int d_head,
                                  int64_t max_length, int n_cus);

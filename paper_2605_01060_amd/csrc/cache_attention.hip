@@ -16,6 +16,10 @@
 namespace surge {
 namespace {
 
+// Workgroups of a kernel on a CU, by its class (few rows: 16, 32, 64; then tiles of
+// 128) and d_head, that registers and LDS allow.
+constexpr int PLACES[4][3] = {{6, 4, 3}, {4, 3, 2}, {3, 2, 1}, {4, 3, 2}};
+
 // The 16 bytes of codes (d_head 128; 8 or 4 for smaller heads) of a quarter of
 // a key or value.
 template <int DH>
@@ -35,15 +39,17 @@ struct Quarter {
   }
 };
 
-// A unit's rows and keys, from the device's offsets and lengths.
+// A unit of work: a tile of rows of one (sequence, key head), with all of the keys
+// that they see or a part of them.
 struct Unit {
+  int index, kvh, row0;   // row0: first row of the tile, in the sequence
   int64_t seq;
-  int tile, kvh, split;
-  int q_beg, rows;       // first query row of the sequence, rows of its tiles
-  int row0, first, last; // of the tile; first: position that row 0 of the sequence is at
-  int k0, k1;            // keys of the unit
-  int limit;             // keys that the tile's last row sees
-  int slot;
+  int q_beg, rows;        // first query row of the sequence, rows of its tiles
+  int first;              // position that row 0 of the sequence is at
+  int limit;              // keys that the tile's last row sees
+  int k0, k1;             // keys of the unit
+  bool whole;             // these are all of its rows' keys
+  int slot;               // of its part, where not
 };
 
 // Keys that a row sees.
@@ -51,35 +57,129 @@ __device__ __forceinline__ int row_limit(const CacheAttention& a, const Unit& u,
   return a.causal ? u.first + row / a.group + 1 : u.limit;
 }
 
-__device__ __forceinline__ bool unit_of(const CacheAttention& a, int64_t index, Unit* u) {
-  u->split = (int)(index % a.splits);
-  index /= a.splits;
-  u->kvh = (int)(index % a.c.n_kv_heads);
-  index /= a.c.n_kv_heads;
-  u->seq = index % a.c.n_seqs;
-  u->tile = a.tiles - 1 - (int)(index / a.c.n_seqs);  // the last rows see the most keys
+// A value that all lanes of a wave have, in a scalar register.
+template <bool WAVE>
+__device__ __forceinline__ int uniform(int v) {
+  return WAVE ? __builtin_amdgcn_readfirstlane(v) : v;
+}
+
+// The rows and all keys of unit `index` (sequence, key head, tile; the last tile
+// first, whose rows see the most keys).  False: no rows.  WAVE: the index is one
+// for the wave.
+template <bool WAVE>
+__device__ __forceinline__ bool unit_of(const CacheAttention& a, int index, Unit* u) {
+  u->index = index;
+  const int tile = a.tiles - 1 - (int)((unsigned)index % (unsigned)a.tiles);
+  index = (int)((unsigned)index / (unsigned)a.tiles);
+  u->kvh = (int)((unsigned)index % (unsigned)a.c.n_kv_heads);
+  u->seq = (int)((unsigned)index / (unsigned)a.c.n_kv_heads);
   int beg, n;
   if (a.r.cu) {
-    beg = min(max(a.r.cu[u->seq], 0), a.r.n_rows);
-    n = min(max(a.r.cu[u->seq + 1], beg), a.r.n_rows) - beg;
+    beg = min(max(uniform<WAVE>(a.r.cu[u->seq]), 0), a.r.n_rows);
+    n = min(max(uniform<WAVE>(a.r.cu[u->seq + 1]), beg), a.r.n_rows) - beg;
   } else {
     beg = (int)u->seq * a.r.each;
     n = a.r.each;
   }
-  const int length = length_of(a.c, (int)u->seq);
+  const int length = uniform<WAVE>(length_of(a.c, (int)u->seq));
   u->q_beg = beg;
   u->first = length - n;
   u->rows = min(n, a.max_rows) * a.group;
-  u->row0 = u->tile * a.tile_rows;
+  u->row0 = tile * a.tile_rows;
   if (u->row0 >= u->rows) return false;
   const int last = min(u->row0 + a.tile_rows, u->rows) - 1;
   u->limit = a.causal ? max(u->first + last / a.group + 1, 0) : length;
-  u->k0 = u->split * a.chunk;
-  u->k1 = min(u->k0 + a.chunk, u->limit);
-  if (u->split > 0 && u->k0 >= u->limit) return false;
-  u->slot = (int)(((u->seq * a.tiles + u->tile) * a.c.n_kv_heads + u->kvh) * a.splits + u->split);
+  u->k0 = 0;
+  u->k1 = u->limit;
+  u->whole = true;
+  u->slot = 0;
   return true;
 }
+
+// Blocks of a unit's keys, one at least where it has rows.
+template <bool WAVE>
+__device__ __forceinline__ int blocks_of(const CacheAttention& a, int index) {
+  Unit u;
+  return unit_of<WAVE>(a, index, &u) ? max((u.limit + a.block_keys - 1) / a.block_keys, 1) : 0;
+}
+
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(v, o, 64);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+
+// A unit a workgroup, or with SHARED the workgroup's equal share of all units'
+// blocks of keys: a share starts and ends anywhere, the parts of a unit that is cut are
+// joined afterwards.  Workgroups of one XCD have shares next to each other, whose
+// units share keys.
+template <bool SHARED, class Body>
+__device__ __forceinline__ void for_units(const CacheAttention& a, Body body) {
+  Unit u;
+  if constexpr (!SHARED) {
+    if (unit_of<true>(a, blockIdx.x, &u)) body(u);
+    return;
+  }
+  __shared__ int s_before[256], s_wave[4];  // blocks before a thread's units
+  const int worker = (int)(blockIdx.x % 8) * (a.workers / 8) + (int)(blockIdx.x / 8);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = (a.units + 255) / 256;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int index = (int)threadIdx.x * per + i;
+    if (index < a.units) mine += blocks_of<false>(a, index);
+  }
+  const int upto = wave_scan(mine);
+  if (lane == 63) s_wave[wave] = upto;
+  __syncthreads();
+  int before = upto - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += s_wave[w];
+    total += s_wave[w];
+  }
+  s_before[threadIdx.x] = before;
+  __syncthreads();
+  total = uniform<true>(total);
+  const int share = max((total + a.workers - 1) / a.workers, a.least_share);
+  int at = worker * share;
+  const int end = min(at + share, total);
+  if (at >= end) return;
+  // The last thread whose units start at or before `at`, then the unit.
+  int thread = -1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) thread += __popcll(__ballot(s_before[i * 64 + lane] <= at));
+  thread = __builtin_amdgcn_readfirstlane(thread);
+  int index = thread * per, start = uniform<true>(s_before[thread]);
+  while (at < end) {
+    const int n = blocks_of<true>(a, index);
+    if (at >= start + n) {
+      start += n;
+      ++index;
+      continue;
+    }
+    unit_of<true>(a, index, &u);
+    const int from = at - start, to = min(n, end - start);
+    u.whole = from == 0 && to == n;
+    u.k0 = from * a.block_keys;
+    u.k1 = min(to * a.block_keys, u.limit);
+    u.slot = 2 * worker + (from == 0);
+    body(u);
+    // Who has a unit's last part knows where it started.
+    if (to == n && threadIdx.x == 0)
+      a.joins[index] = make_int2(u.whole ? -1 : start / share, worker);
+    at = start + to;
+    if (at < end) __syncthreads();  // LDS is read out
+  }
+}
+
+// The slot of part p of a unit that is joined: its first worker has its head,
+// the others' first parts are its.
+__device__ __forceinline__ int part_slot(int2 join, int p) { return 2 * (join.x + p) + (p == 0); }
 
 // A lane's value combined with those of the lanes 16 and 32 apart.
 template <class Op>
@@ -155,14 +255,12 @@ __device__ __forceinline__ uint32_t v_slot(int key, int chunk) {
 // Few rows: RT tiles of 16 against blocks of 32 keys, each wave of four with
 // blocks of its own.
 template <int DH, int RT>
-__global__ __launch_bounds__(256) void few_rows_kernel(CacheAttention a) {
+__device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Unit& u) {
   constexpr int STEPS = DH / 32, FT = DH / 16, CPR = DH / 8, WAVES = 4;
   constexpr int STRIDE = DH + 4;  // floats of a staged output row
   constexpr int LDS_WAVE = (32 * DH * 2 > 16 * STRIDE * 4 ? 32 * DH * 2 : 16 * STRIDE * 4);
   __shared__ __attribute__((aligned(256))) uint8_t lds[WAVES * LDS_WAVE];
   __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
-  Unit u;
-  if (!unit_of(a, blockIdx.x, &u)) return;
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.group;
@@ -292,7 +390,6 @@ __global__ __launch_bounds__(256) void few_rows_kernel(CacheAttention a) {
     }
   }
   __syncthreads();
-  const bool whole = a.splits == 1 || u.limit <= a.chunk;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float m = s_m[0][rt * 16 + col];
@@ -321,7 +418,7 @@ __global__ __launch_bounds__(256) void few_rows_kernel(CacheAttention a) {
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
           v += *reinterpret_cast<const f32x4*>(lds + w * LDS_WAVE + (r * STRIDE + d) * 4);
-        if (whole) {
+        if (u.whole) {
           uint2 out;
           out.x = seen ? pack_bf16x2(v[0] * inv, v[1] * inv) : 0u;
           out.y = seen ? pack_bf16x2(v[2] * inv, v[3] * inv) : 0u;
@@ -358,13 +455,11 @@ __device__ __forceinline__ float over_halves(float v, float (*op)(float, float))
 }
 
 template <int DH>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void tile_kernel(CacheAttention a) {
+__device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u) {
   using L = PageLayout<DH>;
   constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8, STEPS = DH / 32, KB = 64, T = KB / 32;
   constexpr uint32_t ROW = DH * 2, BUF = KB * ROW;
   __shared__ __attribute__((aligned(256))) u32x4 sKV[4 * BUF / 16];  // K blocks by parity, then V blocks
-  Unit u;
-  if (!unit_of(a, blockIdx.x, &u)) return;
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.group;
@@ -521,7 +616,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
   const bool seen = limit > u.k0;
 
   // Register r of tile dt: feature dt 32 + 8 (r / 4) + 4 half + r % 4 of row col.
-  if (a.splits == 1 || u.limit <= a.chunk) {
+  if (u.whole) {
     __syncthreads();  // every wave has read its last block
     if (!active) return;
     const float inv = 1.0f / l_run;
@@ -559,38 +654,86 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void t
           make_float4(o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]);
 }
 
-// Joins the parts of a row of one key head: a wave a row, in the order of the
-// keys.
-template <int DH>
-__global__ __launch_bounds__(256) void join_kernel(CacheAttention a) {
+template <int DH, int RT, bool SHARED>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(PLACES[RT / 2][DH / 64]))) void few_rows_kernel(CacheAttention a) {
+  for_units<SHARED>(a, [&](const Unit& u) { few_rows_unit<DH, RT>(a, u); });
+}
+
+template <int DH, bool SHARED>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(PLACES[3][DH / 64]))) void tile_kernel(CacheAttention a) {
+  for_units<SHARED>(a, [&](const Unit& u) { tile_unit<DH>(a, u); });
+}
+
+// Joins the parts of a row: WAVES waves take parts w, w + WAVES, ..., BATCH loads
+// in flight, and are added in order.  A workgroup has ROWS rows of a unit.
+template <int DH, int WAVES, int ROWS, int BATCH>
+__global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention a, int row_groups) {
   constexpr int PER = DH < 64 ? 1 : DH / 64;
+  static_assert(WAVES == 1 || ROWS == 1, "waves that meet have one row");
+  __shared__ float sm[WAVES], so[WAVES][DH + 1];
   const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = (int)(wave % a.tile_rows);
+  const int wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+  const int index = (int)(blockIdx.x / (unsigned)row_groups);
+  const int r = (int)(blockIdx.x % (unsigned)row_groups) * ROWS +
+                (WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
   Unit u;
-  if (!unit_of(a, wave / a.tile_rows * a.splits, &u)) return;
-  const int row = u.row0 + r;
-  if (u.limit <= a.chunk || row >= u.rows) return;
-  const int parts = (u.limit + a.chunk - 1) / a.chunk;
-  auto slot = [&](int p) { return (int64_t)(u.slot + p) * a.tile_rows + r; };
+  if (!unit_of<true>(a, index, &u) || u.row0 + r >= u.rows || r >= a.tile_rows) return;
+  const int2 join = a.joins[index];
+  if (join.x < 0) return;
+  const int parts = join.y - join.x + 1;
+  auto slot = [&](int p) { return (int64_t)part_slot(join, p) * a.tile_rows + r; };
   float m = -INFINITY;
-  for (int p = lane; p < parts; p += 64) m = fmaxf(m, a.part_ml[slot(p)].x);
+  for (int p = wave * 64 + lane; p < parts; p += 64 * WAVES) m = fmaxf(m, a.part_ml[slot(p)].x);
   m = wave_max(m);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) sm[wave] = m;
+    __syncthreads();
+    m = sm[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w]);
+  }
   float l = 0.0f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-  // Without any key for the row every part is zeros: nothing to add.
-#pragma unroll 4
-  for (int p = 0; p < (m > -INFINITY ? parts : 0); ++p) {
-    const float2 ml = a.part_ml[slot(p)];
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    l = fmaf(f, ml.y, l);
+  // Without any key for the row (m = -inf) every part is zeros: nothing to add.
+  for (int p0 = wave; p0 < parts && m > -INFINITY; p0 += WAVES * BATCH) {
+    float2 ml[BATCH];
+    float v[BATCH][PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (lane < DH) o[i] = fmaf(f, a.part_o[slot(p) * DH + lane * PER + i], o[i]);
+    for (int q = 0; q < BATCH; ++q) {
+      const int64_t s = slot(min(p0 + q * WAVES, parts - 1));
+      ml[q] = a.part_ml[s];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) v[q][i] = lane < DH ? a.part_o[s * DH + lane * PER + i] : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      const bool on = p0 + q * WAVES < parts;
+      const float f = on ? __builtin_amdgcn_exp2f(ml[q].x - m) : 0.0f;
+      l = fmaf(f, on ? ml[q].y : 0.0f, l);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) o[i] = fmaf(f, on ? v[q][i] : 0.0f, o[i]);
+    }
+  }
+  if constexpr (WAVES > 1) {
+    if (lane == 0) so[wave][DH] = l;
+    if (lane < DH)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) so[wave][lane * PER + i] = o[i];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      l += so[w][DH];
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (lane < DH) o[i] += so[w][lane * PER + i];
+    }
   }
   const float inv = m > -INFINITY ? 1.0f / l : 0.0f;
-  const int G = a.group;
+  const int row = u.row0 + r, G = a.group;
   uint16_t* out = a.out + (int64_t)(u.q_beg + row / G) * a.ld_out + (u.kvh * G + row % G) * DH;
   if constexpr (PER == 2)
     reinterpret_cast<uint32_t*>(out)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
@@ -600,14 +743,29 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttention a) {
 
 template <int DH>
 hipError_t launch(const CacheAttention& a, hipStream_t stream) {
-  const int64_t tiles = (int64_t)a.tiles * a.c.n_seqs * a.c.n_kv_heads;
-  const dim3 grid((unsigned)(tiles * a.splits)), block(256);
-  if (a.tile_rows == 16) hipLaunchKernelGGL((few_rows_kernel<DH, 1>), grid, block, 0, stream, a);
-  if (a.tile_rows == 32) hipLaunchKernelGGL((few_rows_kernel<DH, 2>), grid, block, 0, stream, a);
-  if (a.tile_rows == 64) hipLaunchKernelGGL((few_rows_kernel<DH, 4>), grid, block, 0, stream, a);
-  if (a.tile_rows == 128) hipLaunchKernelGGL(tile_kernel<DH>, grid, block, 0, stream, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL(join_kernel<DH>, dim3((unsigned)(tiles * a.tile_rows / 4)), block, 0, stream, a);
+  const dim3 grid(a.workers ? a.workers : a.units), block(256);
+#define SURGE_LAUNCH(...)                                                                  \
+  do {                                                                                     \
+    if (a.workers)                                                                         \
+      hipLaunchKernelGGL((__VA_ARGS__, true>), grid, block, 0, stream, a);                 \
+    else                                                                                   \
+      hipLaunchKernelGGL((__VA_ARGS__, false>), grid, block, 0, stream, a);                \
+  } while (0)
+  if (a.tile_rows == 16) SURGE_LAUNCH(few_rows_kernel<DH, 1);
+  if (a.tile_rows == 32) SURGE_LAUNCH(few_rows_kernel<DH, 2);
+  if (a.tile_rows == 64) SURGE_LAUNCH(few_rows_kernel<DH, 4);
+  if (a.tile_rows == 128) SURGE_LAUNCH(tile_kernel<DH);
+#undef SURGE_LAUNCH
+  if (a.workers == 0) return hipGetLastError();
+  const int rows = (int)std::min<int64_t>(a.tile_rows, (int64_t)a.max_rows * a.group);
+  if (a.workers >= 16 * a.units) {
+    hipLaunchKernelGGL((join_kernel<DH, 16, 1, 8>), dim3(a.units * rows), dim3(1024), 0, stream, a, rows);
+  } else if (a.workers >= 4 * a.units) {
+    hipLaunchKernelGGL((join_kernel<DH, 4, 1, 8>), dim3(a.units * rows), dim3(256), 0, stream, a, rows);
+  } else {
+    const int groups = (rows + 3) / 4;
+    hipLaunchKernelGGL((join_kernel<DH, 1, 4, 4>), dim3(a.units * groups), dim3(256), 0, stream, a, groups);
+  }
   return hipGetLastError();
 }
 
@@ -617,13 +775,17 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
                                  int64_t max_length, int n_cus) {
   CacheShape s;
   const int64_t rows = max_rows * group;
-  s.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  const int cls = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+  s.tile_rows = 16 << cls;
+  if (cls == 3) s.tile_rows = 128;
+  s.block_keys = cls == 3 ? 64 : 128;  // few rows: 32 for each wave
   s.tiles = (rows + s.tile_rows - 1) / s.tile_rows;
-  const int64_t units = n_seqs * n_kv_heads * s.tiles;
-  const int64_t want = std::max<int64_t>(1, 4 * (int64_t)n_cus / units);
-  // Whole rounds of blocks of the four waves.
-  s.chunk = std::max<int64_t>(256, ((max_length + want - 1) / want + 127) / 128 * 128);
-  s.splits = std::max<int64_t>(1, (max_length + s.chunk - 1) / s.chunk);
+  s.units = n_seqs * n_kv_heads * s.tiles;
+  const int64_t workers = (int64_t)n_cus * PLACES[cls][d_head / 64] / 8 * 8;
+  const int64_t most = (max_length + s.block_keys - 1) / s.block_keys;  // blocks of a unit
+  s.least_share = 2;
+  s.workers = 0;
+  if (most > 2 && s.units <= 8192 && s.units * most < INT32_MAX && s.units <= 4 * workers) s.workers = workers;
   return s;
 }
 

@@ -117,10 +117,10 @@ surge_status attention_shape(const surge_kv_cache* c, int64_t max_rows, int32_t 
                              CacheShape* s, int64_t* bytes) {
   *s = cache_attention_shape(c->n_seqs, max_rows, c->n_kv_heads, n_heads / c->n_kv_heads, c->d_head,
                              c->max_length, n_cus);
-  const int64_t tiles = s->tiles * c->n_seqs * c->n_kv_heads;
-  if (tiles * std::max<int64_t>(s->splits, (s->tile_rows + 3) / 4) > kMostThreads / 256)
+  // Threads of the units' launch and, where they are joined, of a wave a row.
+  if (s->units > kMostThreads / 256 || (s->workers && s->units * s->tile_rows > kMostThreads / 64))
     return fail(SURGE_ERR_CAPACITY, "too many rows, heads and sequences for one call");
-  *bytes = s->splits > 1 ? tiles * s->splits * s->tile_rows * (8 + 4 * (int64_t)c->d_head) : 0;
+  *bytes = s->workspace_bytes(c->d_head);
   return SURGE_OK;
 }
 
@@ -218,12 +218,14 @@ surge_status surge_op_cache_attention(const surge_kv_cache* cache, int64_t n_row
   a.causal = causal != 0;
   a.scale_log2 = scale_log2;
   a.tile_rows = s.tile_rows;
+  a.block_keys = s.block_keys;
   a.tiles = (int)s.tiles;
-  a.splits = (int)s.splits;
-  a.chunk = (int)s.chunk;
+  a.units = (int)s.units;
+  a.workers = (int)s.workers;
+  a.least_share = s.least_share;
   a.part_o = (float*)d_workspace;
-  a.part_ml = (float2*)((float*)d_workspace +
-                        s.tiles * cache->n_seqs * cache->n_kv_heads * s.splits * s.tile_rows * cache->d_head);
+  a.part_ml = (float2*)(a.part_o + s.slot_rows() * cache->d_head);
+  a.joins = (int2*)(a.part_ml + s.slot_rows());
   HIP_TRY(launch_cache_attention(a, cache->d_head, (hipStream_t)hip_stream));
   return SURGE_OK;
 }
