@@ -36,6 +36,13 @@ struct CacheStore {
 hipError_t launch_cache_write(const CacheStore& a, int d_head, hipStream_t stream);
 hipError_t launch_cache_read(const CacheStore& a, int d_head, hipStream_t stream);
 
+// What a kernel divides a number below 2^31 by d with.
+struct Divisor {
+  uint32_t m;
+  int s;
+};
+Divisor divisor(int d);  // d >= 1
+
 struct CacheAttention {
   CacheView c;
   CacheRows r;
@@ -46,7 +53,8 @@ struct CacheAttention {
   bool causal;
   float scale_log2;   // scale * log2(e)
   // Of cache_attention_shape.
-  int tile_rows, block_keys, tiles, units, workers, least_share;
+  int tile_rows, block_shift, tiles, units, workers, least_share;
+  Divisor by_group, by_tiles, by_heads, by_units;  // by_units: by n_seqs * n_kv_heads
   // Workspace, where there are workers: of the two slots that each has for the
   // parts of its first and last unit, the rows' maxima (in log2 units) and sums,
   // their outputs, and which workers have the parts of a unit.
@@ -57,10 +65,10 @@ struct CacheAttention {
 
 // How a call is cut into units: tiles of tile_rows rows (query * group + head
 // of the group) of each (sequence, key head).  Their keys, in blocks of
-// block_keys, are shared out to `workers` workgroups, at least least_share blocks
+// 1 << block_shift, are shared out to `workers` workgroups, at least least_share blocks
 // each, or where that is 0 a unit is a workgroup's.
 struct CacheShape {
-  int tile_rows, block_keys, least_share;
+  int tile_rows, block_shift, least_share;
   int64_t tiles, units, workers;
   int64_t slot_rows() const { return 2 * workers * tile_rows; }
   int64_t workspace_bytes(int d_head) const {

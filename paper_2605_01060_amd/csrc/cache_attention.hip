@@ -16,9 +16,8 @@
 namespace surge {
 namespace {
 
-// Workgroups of a kernel on a CU, by its class (few rows: 16, 32, 64; then tiles of
-// 128) and d_head, that registers and LDS allow.
-constexpr int PLACES[4][3] = {{6, 4, 3}, {4, 3, 2}, {3, 2, 1}, {4, 3, 2}};
+// Workgroups of a kernel on a CU, by its class (few rows: 16, 32; tiles of 64, 128) and d_head, that registers and LDS allow.
+constexpr int PLACES[4][3] = {{5, 4, 3}, {4, 3, 2}, {4, 3, 2}, {4, 3, 2}};
 
 // The 16 bytes of codes (d_head 128; 8 or 4 for smaller heads) of a quarter of
 // a key or value.
@@ -39,101 +38,122 @@ struct Quarter {
   }
 };
 
+// x / d for x < 2^31: m = ceil(2^(31 + s) / d) with 2^s >= d is off from 2^(31 + s) /
+// d by less than 2^-31 of it.
+__device__ __forceinline__ int over(int x, const Divisor& d) {
+  return (int)(__umulhi((uint32_t)x << 1, d.m) >> d.s);
+}
+
+// A sequence's rows: the first one's number and position, how many there are
+// (queries * group), and the sequence's length.
+struct Sequence {
+  int q_beg, rows, first, length;
+};
+
+__device__ __forceinline__ Sequence sequence_of(const CacheAttention& a, int seq) {
+  Sequence s;
+  int n;
+  if (a.r.cu) {
+    s.q_beg = min(max(a.r.cu[seq], 0), a.r.n_rows);
+    n = min(max(a.r.cu[seq + 1], s.q_beg), a.r.n_rows) - s.q_beg;
+  } else {
+    s.q_beg = seq * a.r.each;
+    n = a.r.each;
+  }
+  s.length = length_of(a.c, seq);
+  s.first = s.length - n;
+  s.rows = min(n, a.max_rows) * a.group;
+  return s;
+}
+
+// A value that all lanes of a wave have, in a scalar register.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ Sequence uniform(const Sequence& s) {
+  return {uniform(s.q_beg), uniform(s.rows), uniform(s.first), uniform(s.length)};
+}
+
 // A unit of work: a tile of rows of one (sequence, key head), with all of the keys
 // that they see or a part of them.
 struct Unit {
-  int index, kvh, row0;   // row0: first row of the tile, in the sequence
-  int64_t seq;
-  int q_beg, rows;        // first query row of the sequence, rows of its tiles
-  int first;              // position that row 0 of the sequence is at
-  int limit;              // keys that the tile's last row sees
-  int k0, k1;             // keys of the unit
-  bool whole;             // these are all of its rows' keys
-  int slot;               // of its part, where not
+  int seq, kvh, row0;         // row0: first row of the tile, in the sequence
+  int q_beg, rows, first;     // of the sequence
+  int limit;                  // keys that the tile's last row sees
+  int k0, k1;                 // keys of the unit
+  bool whole;                 // these are all of its rows' keys
+  int slot;                   // of its part, where not
 };
 
 // Keys that a row sees.
 __device__ __forceinline__ int row_limit(const CacheAttention& a, const Unit& u, int row) {
-  return a.causal ? u.first + row / a.group + 1 : u.limit;
+  return a.causal ? u.first + over(row, a.by_group) + 1 : u.limit;
 }
 
-// A value that all lanes of a wave have, in a scalar register.
-template <bool WAVE>
-__device__ __forceinline__ int uniform(int v) {
-  return WAVE ? __builtin_amdgcn_readfirstlane(v) : v;
+// Keys that the last row of tile `tile` sees; blocks of them, one at least, 0 for
+// a tile without rows.
+__device__ __forceinline__ int limit_of(const CacheAttention& a, const Sequence& s, int tile) {
+  const int last = min((tile + 1) * a.tile_rows, s.rows) - 1;
+  return a.causal ? max(s.first + over(last, a.by_group) + 1, 0) : s.length;
+}
+__device__ __forceinline__ int blocks_of(const CacheAttention& a, const Sequence& s, int tile) {
+  if (tile * a.tile_rows >= s.rows) return 0;
+  return max((limit_of(a, s, tile) + (1 << a.block_shift) - 1) >> a.block_shift, 1);
 }
 
-// The rows and all keys of unit `index` (sequence, key head, tile; the last tile
-// first, whose rows see the most keys).  False: no rows.  WAVE: the index is one
-// for the wave.
-template <bool WAVE>
-__device__ __forceinline__ bool unit_of(const CacheAttention& a, int index, Unit* u) {
-  u->index = index;
-  const int tile = a.tiles - 1 - (int)((unsigned)index % (unsigned)a.tiles);
-  index = (int)((unsigned)index / (unsigned)a.tiles);
-  u->kvh = (int)((unsigned)index % (unsigned)a.c.n_kv_heads);
-  u->seq = (int)((unsigned)index / (unsigned)a.c.n_kv_heads);
-  int beg, n;
-  if (a.r.cu) {
-    beg = min(max(uniform<WAVE>(a.r.cu[u->seq]), 0), a.r.n_rows);
-    n = min(max(uniform<WAVE>(a.r.cu[u->seq + 1]), beg), a.r.n_rows) - beg;
-  } else {
-    beg = (int)u->seq * a.r.each;
-    n = a.r.each;
-  }
-  const int length = uniform<WAVE>(length_of(a.c, (int)u->seq));
-  u->q_beg = beg;
-  u->first = length - n;
-  u->rows = min(n, a.max_rows) * a.group;
-  u->row0 = tile * a.tile_rows;
-  if (u->row0 >= u->rows) return false;
-  const int last = min(u->row0 + a.tile_rows, u->rows) - 1;
-  u->limit = a.causal ? max(u->first + last / a.group + 1, 0) : length;
-  u->k0 = 0;
-  u->k1 = u->limit;
-  u->whole = true;
-  u->slot = 0;
-  return true;
-}
-
-// Blocks of a unit's keys, one at least where it has rows.
-template <bool WAVE>
-__device__ __forceinline__ int blocks_of(const CacheAttention& a, int index) {
+// With all of its keys.
+__device__ __forceinline__ Unit unit_of(const CacheAttention& a, const Sequence& s, int seq, int kvh, int tile) {
   Unit u;
-  return unit_of<WAVE>(a, index, &u) ? max((u.limit + a.block_keys - 1) / a.block_keys, 1) : 0;
+  u.seq = seq;
+  u.kvh = kvh;
+  u.row0 = tile * a.tile_rows;
+  u.q_beg = s.q_beg;
+  u.rows = s.rows;
+  u.first = s.first;
+  u.limit = limit_of(a, s, tile);
+  u.k0 = 0;
+  u.k1 = u.limit;
+  u.whole = true;
+  u.slot = 0;
+  return u;
 }
 
-__device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(v, o, 64);
-    if (lane >= o) v += x;
-  }
-  return v;
+__device__ __forceinline__ int scan64(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // of lanes 1, 2, 4, 8 before in a row
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);  // of the last lane of the row, the half before
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
 }
 
-// A unit a workgroup, or with SHARED the workgroup's equal share of all units'
-// blocks of keys: a share starts and ends anywhere, the parts of a unit that is cut are
-// joined afterwards.  Workgroups of one XCD have shares next to each other, whose
-// units share keys.
-template <bool SHARED, class Body>
-__device__ __forceinline__ void for_units(const CacheAttention& a, Body body) {
-  Unit u;
-  if constexpr (!SHARED) {
-    if (unit_of<true>(a, blockIdx.x, &u)) body(u);
-    return;
-  }
-  __shared__ int s_before[256], s_wave[4];  // blocks before a thread's units
+// A unit a workgroup, the last tiles first, whose rows see the most keys.
+template <class Body>
+__device__ __forceinline__ void one_unit(const CacheAttention& a, Body body) {
+  const int index = blockIdx.x, of_tile = over(index, a.by_units);
+  const int rest = index - of_tile * (a.c.n_seqs * a.c.n_kv_heads), tile = a.tiles - 1 - of_tile;
+  const int seq = over(rest, a.by_heads);
+  const Sequence s = uniform(sequence_of(a, seq));
+  if (tile * a.tile_rows < s.rows) body(unit_of(a, s, seq, rest - seq * a.c.n_kv_heads, tile));
+}
+
+// The workgroup's equal share of all units' blocks of keys, in the order of
+// sequence, key head, tile: it starts and ends anywhere, and the parts of a unit
+// that is cut are joined afterwards.  Workgroups of one XCD have shares next to each
+// other, whose units share keys.
+template <class Body>
+__device__ __forceinline__ void shared_units(const CacheAttention& a, Body body) {
+  __shared__ int s_before[256], s_wave[4];  // blocks before a thread's sequences
   const int worker = (int)(blockIdx.x % 8) * (a.workers / 8) + (int)(blockIdx.x / 8);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (a.units + 255) / 256;
+  const int per = (a.c.n_seqs + 255) >> 8;
+  auto blocks_of_head = [&](const Sequence& s) {
+    int n = 0;
+    for (int t = 0; t < a.tiles; ++t) n += blocks_of(a, s, t);
+    return n;
+  };
   int mine = 0;
-  for (int i = 0; i < per; ++i) {
-    const int index = (int)threadIdx.x * per + i;
-    if (index < a.units) mine += blocks_of<false>(a, index);
-  }
-  const int upto = wave_scan(mine);
+  for (int i = (int)threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, a.c.n_seqs); ++i)
+    mine += blocks_of_head(sequence_of(a, i)) * a.c.n_kv_heads;
+  const int upto = scan64(mine);
   if (lane == 63) s_wave[wave] = upto;
   __syncthreads();
   int before = upto - mine, total = 0;
@@ -144,36 +164,45 @@ __device__ __forceinline__ void for_units(const CacheAttention& a, Body body) {
   }
   s_before[threadIdx.x] = before;
   __syncthreads();
-  total = uniform<true>(total);
+  total = uniform(total);
   const int share = max((total + a.workers - 1) / a.workers, a.least_share);
   int at = worker * share;
   const int end = min(at + share, total);
   if (at >= end) return;
-  // The last thread whose units start at or before `at`, then the unit.
+  // The last thread whose sequences start at or before `at`, then the sequence,
+  // its key head and tile.
   int thread = -1;
 #pragma unroll
   for (int i = 0; i < 4; ++i) thread += __popcll(__ballot(s_before[i * 64 + lane] <= at));
-  thread = __builtin_amdgcn_readfirstlane(thread);
-  int index = thread * per, start = uniform<true>(s_before[thread]);
-  while (at < end) {
-    const int n = blocks_of<true>(a, index);
-    if (at >= start + n) {
-      start += n;
-      ++index;
+  int seq = uniform(thread) * per, start = uniform(s_before[uniform(thread)]);
+  for (; at < end; ++seq) {
+    const Sequence s = uniform(sequence_of(a, seq));
+    const int n_head = uniform(blocks_of_head(s));
+    if (at >= start + n_head * a.c.n_kv_heads) {
+      start += n_head * a.c.n_kv_heads;
       continue;
     }
-    unit_of<true>(a, index, &u);
-    const int from = at - start, to = min(n, end - start);
-    u.whole = from == 0 && to == n;
-    u.k0 = from * a.block_keys;
-    u.k1 = min(to * a.block_keys, u.limit);
-    u.slot = 2 * worker + (from == 0);
-    body(u);
-    // Who has a unit's last part knows where it started.
-    if (to == n && threadIdx.x == 0)
-      a.joins[index] = make_int2(u.whole ? -1 : start / share, worker);
-    at = start + to;
-    if (at < end) __syncthreads();  // LDS is read out
+    const int past = (at - start) / n_head;
+    start += past * n_head;
+    for (int kvh = past; kvh < a.c.n_kv_heads && at < end; ++kvh)
+      for (int tile = 0; tile < a.tiles && at < end; ++tile) {
+        const int n = blocks_of(a, s, tile);
+        if (at < start + n) {
+          Unit u = unit_of(a, s, seq, kvh, tile);
+          const int from = at - start, to = min(n, end - start);
+          u.whole = from == 0 && to == n;
+          u.k0 = from << a.block_shift;
+          u.k1 = min(to << a.block_shift, u.limit);
+          u.slot = 2 * worker + (from == 0);
+          body(u);
+          // Who has a unit's last part knows where it started.
+          if (to == n && threadIdx.x == 0)
+            a.joins[(seq * a.c.n_kv_heads + kvh) * a.tiles + tile] = make_int2(u.whole ? -1 : start / share, worker);
+          at = start + to;
+          if (at < end) __syncthreads();  // LDS is read out
+        }
+        start += n;
+      }
   }
 }
 
@@ -259,7 +288,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
   constexpr int STEPS = DH / 32, FT = DH / 16, CPR = DH / 8, WAVES = 4;
   constexpr int STRIDE = DH + 4;  // floats of a staged output row
   constexpr int LDS_WAVE = (32 * DH * 2 > 16 * STRIDE * 4 ? 32 * DH * 2 : 16 * STRIDE * 4);
-  __shared__ __attribute__((aligned(256))) uint8_t lds[WAVES * LDS_WAVE];
+  __shared__ __attribute__((aligned(256))) uint8_t lds[RT * WAVES * LDS_WAVE];
   __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -271,7 +300,8 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
   for (int rt = 0; rt < RT; ++rt) {
     const int row = min(u.row0 + rt * 16 + col, u.rows - 1);
     limit[rt] = row_limit(a, u, row);
-    const uint16_t* q = a.q + (int64_t)(u.q_beg + row / G) * a.ld_q + (u.kvh * G + row % G) * DH;
+    const int query = over(row, a.by_group);
+    const uint16_t* q = a.q + (int64_t)(u.q_beg + query) * a.ld_q + (u.kvh * G + row - query * G) * DH;
 #pragma unroll
     for (int kk = 0; kk < STEPS; ++kk)
       qf[rt][kk] = *reinterpret_cast<const bf16x8*>(q + quarter * (DH / 4) + kk * 8);
@@ -396,7 +426,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) m = fmaxf(m, s_m[w][rt * 16 + col]);
     const float alpha = __builtin_amdgcn_exp2f(m_ref[rt] - m);
-    float* const stage = reinterpret_cast<float*>(lds + wave * LDS_WAVE) + col * STRIDE + 4 * quarter;
+    float* const stage = reinterpret_cast<float*>(lds + (rt * WAVES + wave) * LDS_WAVE) + col * STRIDE + 4 * quarter;
 #pragma unroll
     for (int f = 0; f < FT; ++f)
       *reinterpret_cast<f32x4*>(stage + 16 * f) =
@@ -417,13 +447,14 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
-          v += *reinterpret_cast<const f32x4*>(lds + w * LDS_WAVE + (r * STRIDE + d) * 4);
+          v += *reinterpret_cast<const f32x4*>(lds + (rt * WAVES + w) * LDS_WAVE + (r * STRIDE + d) * 4);
         if (u.whole) {
           uint2 out;
           out.x = seen ? pack_bf16x2(v[0] * inv, v[1] * inv) : 0u;
           out.y = seen ? pack_bf16x2(v[2] * inv, v[3] * inv) : 0u;
-          *reinterpret_cast<uint2*>(a.out + (int64_t)(u.q_beg + row / G) * a.ld_out +
-                                    (u.kvh * G + row % G) * DH + d) = out;
+          const int query = over(row, a.by_group);
+          *reinterpret_cast<uint2*>(a.out + (int64_t)(u.q_beg + query) * a.ld_out +
+                                    (u.kvh * G + row - query * G) * DH + d) = out;
         } else {
           const int64_t slot = (int64_t)u.slot * a.tile_rows + rt * 16 + r;
           *reinterpret_cast<f32x4*>(a.part_o + slot * DH + d) = v;
@@ -431,13 +462,13 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
         }
       }
     }
-    __syncthreads();
   }
 }
 
-// Many rows: four waves of 32 share blocks of 64 keys in LDS, decoded to bf16 by
-// all of them, each wave a tile of 16 keys.  A block's codes are loaded two blocks
-// ahead and decoded one ahead.
+// Many rows: four waves share blocks of 64 keys in LDS, decoded to bf16 by all of
+// them, each wave a tile of 16 keys.  A block's codes are loaded two blocks ahead
+// and decoded one ahead.  With GROUPS = 4 a wave has 32 rows against the whole block,
+// with 2 against half of it, and the halves are joined in the end.
 //
 // Chunk c of row r is stored at c ^ f(r), so that neither the reads of K (a chunk
 // of 32 rows), the transposing reads of V (64 bytes of four consecutive rows) nor,
@@ -454,16 +485,17 @@ __device__ __forceinline__ float over_halves(float v, float (*op)(float, float))
   return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int DH>
+template <int DH, int GROUPS>
 __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u) {
   using L = PageLayout<DH>;
-  constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8, STEPS = DH / 32, KB = 64, T = KB / 32;
+  constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8, STEPS = DH / 32, KB = 64, T = GROUPS / 2;  // T: 32-key tiles of a wave
   constexpr uint32_t ROW = DH * 2, BUF = KB * ROW;
   __shared__ __attribute__((aligned(256))) u32x4 sKV[4 * BUF / 16];  // K blocks by parity, then V blocks
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.group;
-  const int row0 = u.row0 + wave * 32;
+  const int rows_of = wave % GROUPS, key_part = wave / GROUPS;
+  const int row0 = u.row0 + rows_of * 32;
   const bool active = row0 < u.rows;  // a wave without rows still decodes
   const int row = min(row0 + col, u.rows - 1);
   const int limit = min(row_limit(a, u, row), u.k1);
@@ -471,7 +503,8 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   const int most_keys = min(row_limit(a, u, min(row0 + 31, u.rows - 1)), u.k1);   // that some row sees
 
   bf16x8 qf[KSTEPS];
-  const uint16_t* q = a.q + (int64_t)(u.q_beg + row / G) * a.ld_q + (u.kvh * G + row % G) * DH;
+  const int query = over(row, a.by_group);
+  const uint16_t* q = a.q + (int64_t)(u.q_beg + query) * a.ld_q + (u.kvh * G + row - query * G) * DH;
 #pragma unroll
   for (int kk = 0; kk < KSTEPS; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(q + (kk * 2 + half) * 8);
 
@@ -482,7 +515,7 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   auto pages_from = [&](int first) {
     const int key = u.k0 + (first + lane) * KB + 16 * wave;
     if (key >= u.k1) return 0;
-    const int page = a.c.table[u.seq * a.c.ld_table + (key >> shift)];
+    const int page = a.c.table[(int64_t)u.seq * a.c.ld_table + (key >> shift)];
     return page >= 0 && page < a.c.n_pages ? page : -1;
   };
   int pages = n > 0 ? pages_from(0) : 0;
@@ -516,8 +549,8 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   const uint32_t lds = lds_address(sKV);
   const int tr_key = 4 * half + ((lane & 15) >> 2);
   const int tr_feat = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  uint32_t ka = lds + kv_position<CPR>(col, half) * 16u;
-  uint32_t va = lds + 2 * BUF + kv_position<CPR>(tr_key, tr_feat >> 3) * 16u + (tr_feat & 7) * 2u;
+  uint32_t ka = lds + key_part * 32 * ROW + kv_position<CPR>(col, half) * 16u;
+  uint32_t va = lds + key_part * 32 * ROW + 2 * BUF + kv_position<CPR>(tr_key, tr_feat >> 3) * 16u + (tr_feat & 7) * 2u;
   constexpr uint32_t H_SWZ = CPR == 4 ? 16 : 32;  // of 8 keys further on
   auto k_fragment = [&](int t, int kk) {
     return __builtin_bit_cast(
@@ -552,7 +585,7 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
       decode(i + 1);
       if (i + 2 < n) load(i + 2);
     }
-    const int key0 = u.k0 + i * KB;
+    const int key0 = u.k0 + i * KB + key_part * 32;
     if (active && key0 < most_keys) {
       f32x16 s[T];
 #pragma unroll
@@ -564,7 +597,7 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
 #pragma unroll
         for (int t = 0; t < T; ++t)
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
-      if (key0 + KB > least) {
+      if (key0 + 32 * T > least) {
         const int seen = limit - key0 - 4 * half;
 #pragma unroll
         for (int r = 0; r < 16 * T; ++r)
@@ -614,13 +647,41 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   }
   l_run = over_halves(l_run, sum_of);
   const bool seen = limit > u.k0;
+  __syncthreads();  // every wave has read its last block
+  if constexpr (GROUPS == 2) {
+    f32x4* const from = reinterpret_cast<f32x4*>(sKV) + rows_of * (32 * DH / 4) + lane;
+    float2* const ml = reinterpret_cast<float2*>(sKV + 2 * (BUF / 16)) + rows_of * 64 + lane;
+    if (key_part == 1) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          from[(dt * 4 + g) * 64] = f32x4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
+      *ml = make_float2(m_ref, l_run);
+    }
+    __syncthreads();
+    if (key_part == 1 || !active) return;
+    const float2 other = *ml;
+    const float m = fmaxf(m_ref, other.x);
+    const float f = __builtin_amdgcn_exp2f(m_ref - m), g2 = __builtin_amdgcn_exp2f(other.x - m);
+    m_ref = m;
+    l_run = l_run * f + other.y * g2;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = from[(dt * 4 + g) * 64];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[dt][4 * g + r] = o[dt][4 * g + r] * f + v[r] * g2;
+      }
+  }
+  if (!active) return;
 
   // Register r of tile dt: feature dt 32 + 8 (r / 4) + 4 half + r % 4 of row col.
   if (u.whole) {
-    __syncthreads();  // every wave has read its last block
-    if (!active) return;
     const float inv = 1.0f / l_run;
-    u32x4* stage = sKV + wave * (32 * CPR);
+    // (Behind what the halves' join still reads and beside its maxima.)
+    u32x4* const stage = sKV + (GROUPS == 2 ? 3 * (BUF / 16) : 0) + rows_of * (32 * CPR);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -635,15 +696,17 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
     for (int j = 0; j < CPR / 2; ++j) {
       const int r = j * (64 / CPR) + lane / CPR, chunk = lane % CPR;
       const u32x4 w = stage[kv_position<CPR>(r, chunk)];
-      if (row0 + r < u.rows)
+      if (row0 + r < u.rows) {
+        const int query = over(row0 + r, a.by_group);
         __builtin_nontemporal_store(
-            w, reinterpret_cast<u32x4*>(a.out + (int64_t)(u.q_beg + (row0 + r) / G) * a.ld_out +
-                                        (u.kvh * G + (row0 + r) % G) * DH + chunk * 8));
+            w, reinterpret_cast<u32x4*>(a.out + (int64_t)(u.q_beg + query) * a.ld_out +
+                                        (u.kvh * G + row0 + r - query * G) * DH + chunk * 8));
+      }
     }
     return;
   }
   if (row0 + col >= u.rows) return;
-  const int64_t slot = (int64_t)u.slot * a.tile_rows + wave * 32 + col;
+  const int64_t slot = (int64_t)u.slot * a.tile_rows + rows_of * 32 + col;
   if (half == 0) a.part_ml[slot] = make_float2(seen ? m_ref : -INFINITY, l_run);
   float* po = a.part_o + slot * DH;
 #pragma unroll
@@ -657,13 +720,17 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
 template <int DH, int RT, bool SHARED>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(PLACES[RT / 2][DH / 64]))) void few_rows_kernel(CacheAttention a) {
-  for_units<SHARED>(a, [&](const Unit& u) { few_rows_unit<DH, RT>(a, u); });
+  auto body = [&](const Unit& u) { few_rows_unit<DH, RT>(a, u); };
+  if constexpr (SHARED) shared_units(a, body);
+  else one_unit(a, body);
 }
 
-template <int DH, bool SHARED>
+template <int DH, int GROUPS, bool SHARED>
 __global__ __launch_bounds__(256)
-__attribute__((amdgpu_waves_per_eu(PLACES[3][DH / 64]))) void tile_kernel(CacheAttention a) {
-  for_units<SHARED>(a, [&](const Unit& u) { tile_unit<DH>(a, u); });
+__attribute__((amdgpu_waves_per_eu(PLACES[GROUPS / 2 + 1][DH / 64]))) void tile_kernel(CacheAttention a) {
+  auto body = [&](const Unit& u) { tile_unit<DH, GROUPS>(a, u); };
+  if constexpr (SHARED) shared_units(a, body);
+  else one_unit(a, body);
 }
 
 // Joins the parts of a row: WAVES waves take parts w, w + WAVES, ..., BATCH loads
@@ -678,8 +745,11 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention 
   const int index = (int)(blockIdx.x / (unsigned)row_groups);
   const int r = (int)(blockIdx.x % (unsigned)row_groups) * ROWS +
                 (WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
-  Unit u;
-  if (!unit_of<true>(a, index, &u) || u.row0 + r >= u.rows || r >= a.tile_rows) return;
+  const int head = over(index, a.by_tiles), tile = index - head * a.tiles;
+  const int seq = over(head, a.by_heads), kvh = head - seq * a.c.n_kv_heads;
+  const Sequence s = uniform(sequence_of(a, seq));
+  const int row = tile * a.tile_rows + r;
+  if (row >= s.rows || r >= a.tile_rows) return;
   const int2 join = a.joins[index];
   if (join.x < 0) return;
   const int parts = join.y - join.x + 1;
@@ -733,8 +803,8 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention 
     }
   }
   const float inv = m > -INFINITY ? 1.0f / l : 0.0f;
-  const int row = u.row0 + r, G = a.group;
-  uint16_t* out = a.out + (int64_t)(u.q_beg + row / G) * a.ld_out + (u.kvh * G + row % G) * DH;
+  const int query = over(row, a.by_group), G = a.group;
+  uint16_t* out = a.out + (int64_t)(s.q_beg + query) * a.ld_out + (kvh * G + row - query * G) * DH;
   if constexpr (PER == 2)
     reinterpret_cast<uint32_t*>(out)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
   else if (lane < DH)
@@ -753,8 +823,8 @@ hipError_t launch(const CacheAttention& a, hipStream_t stream) {
   } while (0)
   if (a.tile_rows == 16) SURGE_LAUNCH(few_rows_kernel<DH, 1);
   if (a.tile_rows == 32) SURGE_LAUNCH(few_rows_kernel<DH, 2);
-  if (a.tile_rows == 64) SURGE_LAUNCH(few_rows_kernel<DH, 4);
-  if (a.tile_rows == 128) SURGE_LAUNCH(tile_kernel<DH);
+  if (a.tile_rows == 64) SURGE_LAUNCH(tile_kernel<DH, 2);
+  if (a.tile_rows == 128) SURGE_LAUNCH(tile_kernel<DH, 4);
 #undef SURGE_LAUNCH
   if (a.workers == 0) return hipGetLastError();
   const int rows = (int)std::min<int64_t>(a.tile_rows, (int64_t)a.max_rows * a.group);
@@ -771,21 +841,27 @@ hipError_t launch(const CacheAttention& a, hipStream_t stream) {
 
 }  // namespace
 
+Divisor divisor(int d) {
+  int s = 0;
+  while ((1ll << s) < d) ++s;
+  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+}
+
 CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_heads, int group, int d_head,
                                  int64_t max_length, int n_cus) {
   CacheShape s;
   const int64_t rows = max_rows * group;
   const int cls = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
   s.tile_rows = 16 << cls;
-  if (cls == 3) s.tile_rows = 128;
-  s.block_keys = cls == 3 ? 64 : 128;  // few rows: 32 for each wave
+  s.block_shift = cls >= 2 ? 6 : 7;  // few rows: 32 keys for each wave
   s.tiles = (rows + s.tile_rows - 1) / s.tile_rows;
   s.units = n_seqs * n_kv_heads * s.tiles;
   const int64_t workers = (int64_t)n_cus * PLACES[cls][d_head / 64] / 8 * 8;
-  const int64_t most = (max_length + s.block_keys - 1) / s.block_keys;  // blocks of a unit
-  s.least_share = 2;
+  const int64_t most = ((max_length - 1) >> s.block_shift) + 1;  // blocks of a unit
+  s.least_share = cls >= 2 ? 8 : 2;
   s.workers = 0;
-  if (most > 2 && s.units <= 8192 && s.units * most < INT32_MAX && s.units <= 4 * workers) s.workers = workers;
+  if (most > (cls >= 2 ? 32 : 8) && n_seqs <= 2048 && s.units * most < INT32_MAX && s.units <= 2 * workers)
+    s.workers = workers;
   return s;
 }
 

@@ -218,7 +218,11 @@ surge_status surge_op_cache_attention(const surge_kv_cache* cache, int64_t n_row
   a.causal = causal != 0;
   a.scale_log2 = scale_log2;
   a.tile_rows = s.tile_rows;
-  a.block_keys = s.block_keys;
+  a.block_shift = s.block_shift;
+  a.by_group = divisor(a.group);
+  a.by_tiles = divisor((int)s.tiles);
+  a.by_heads = divisor(cache->n_kv_heads);
+  a.by_units = divisor(cache->n_seqs * cache->n_kv_heads);
   a.tiles = (int)s.tiles;
   a.units = (int)s.units;
   a.workers = (int)s.workers;
