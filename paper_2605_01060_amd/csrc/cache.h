@@ -54,7 +54,7 @@ struct CacheAttention {
   float scale_log2;   // scale * log2(e)
   // Of cache_attention_shape.
   int tile_rows, block_shift, tiles, units, workers, least_share;
-  Divisor by_group, by_tiles, by_heads, by_units;  // by_units: by n_seqs * n_kv_heads
+  Divisor by_group, by_tiles, by_heads, by_units, by_workers;  // by_units: by n_seqs * n_kv_heads
   // Workspace, where there are workers: of the two slots that each has for the
   // parts of its first and last unit, the rows' maxima (in log2 units) and sums,
   // their outputs, and which workers have the parts of a unit.

@@ -142,6 +142,7 @@ __device__ __forceinline__ void one_unit(const CacheAttention& a, Body body) {
 template <class Body>
 __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body) {
   __shared__ int s_before[256], s_wave[4];  // blocks before a thread's sequences
+  __shared__ Sequence s_first[256];         // its first sequence
   const int worker = (int)(blockIdx.x % 8) * (a.workers / 8) + (int)(blockIdx.x / 8);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (a.c.n_seqs + 255) >> 8;
@@ -151,8 +152,13 @@ __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body)
     return n;
   };
   int mine = 0;
-  for (int i = (int)threadIdx.x * per; i < min((int)(threadIdx.x + 1) * per, a.c.n_seqs); ++i)
-    mine += blocks_of_head(sequence_of(a, i)) * a.c.n_kv_heads;
+  for (int i = 0; i < per; ++i) {
+    const int seq = (int)threadIdx.x * per + i;
+    if (seq >= a.c.n_seqs) break;
+    const Sequence s = sequence_of(a, seq);
+    if (i == 0) s_first[threadIdx.x] = s;
+    mine += blocks_of_head(s) * a.c.n_kv_heads;
+  }
   const int upto = scan64(mine);
   if (lane == 63) s_wave[wave] = upto;
   __syncthreads();
@@ -165,7 +171,7 @@ __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body)
   s_before[threadIdx.x] = before;
   __syncthreads();
   total = uniform(total);
-  const int share = max((total + a.workers - 1) / a.workers, a.least_share);
+  const int share = max(over(total + a.workers - 1, a.by_workers), a.least_share);
   int at = worker * share;
   const int end = min(at + share, total);
   if (at >= end) return;
@@ -174,15 +180,16 @@ __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body)
   int thread = -1;
 #pragma unroll
   for (int i = 0; i < 4; ++i) thread += __popcll(__ballot(s_before[i * 64 + lane] <= at));
-  int seq = uniform(thread) * per, start = uniform(s_before[uniform(thread)]);
-  for (; at < end; ++seq) {
-    const Sequence s = uniform(sequence_of(a, seq));
+  thread = uniform(thread);
+  int seq = thread * per, start = uniform(s_before[thread]);
+  for (bool first = true; at < end; ++seq, first = false) {
+    const Sequence s = uniform(first ? s_first[thread] : sequence_of(a, seq));
     const int n_head = uniform(blocks_of_head(s));
     if (at >= start + n_head * a.c.n_kv_heads) {
       start += n_head * a.c.n_kv_heads;
       continue;
     }
-    const int past = (at - start) / n_head;
+    const int past = a.c.n_kv_heads == 1 ? 0 : (at - start) / n_head;
     start += past * n_head;
     for (int kvh = past; kvh < a.c.n_kv_heads && at < end; ++kvh)
       for (int tile = 0; tile < a.tiles && at < end; ++tile) {
@@ -733,8 +740,8 @@ __attribute__((amdgpu_waves_per_eu(PLACES[GROUPS / 2 + 1][DH / 64]))) void tile_
   else one_unit(a, body);
 }
 
-// Joins the parts of a row: WAVES waves take parts w, w + WAVES, ..., BATCH loads
-// in flight, and are added in order.  A workgroup has ROWS rows of a unit.
+// Joins the parts of a row: WAVES waves take parts w, w + WAVES, ..., BATCH of them
+// loaded together, and are added in order.  A workgroup has ROWS rows of a unit.
 template <int DH, int WAVES, int ROWS, int BATCH>
 __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention a, int row_groups) {
   constexpr int PER = DH < 64 ? 1 : DH / 64;
@@ -747,37 +754,35 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention 
                 (WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
   const int head = over(index, a.by_tiles), tile = index - head * a.tiles;
   const int seq = over(head, a.by_heads), kvh = head - seq * a.c.n_kv_heads;
+  const int2 join = a.joins[index];  // (of a tile without rows, whatever stands there)
   const Sequence s = uniform(sequence_of(a, seq));
   const int row = tile * a.tile_rows + r;
   if (row >= s.rows || r >= a.tile_rows) return;
-  const int2 join = a.joins[index];
   if (join.x < 0) return;
   const int parts = join.y - join.x + 1;
-  auto slot = [&](int p) { return (int64_t)part_slot(join, p) * a.tile_rows + r; };
-  float m = -INFINITY;
-  for (int p = wave * 64 + lane; p < parts; p += 64 * WAVES) m = fmaxf(m, a.part_ml[slot(p)].x);
-  m = wave_max(m);
-  if constexpr (WAVES > 1) {
-    if (lane == 0) sm[wave] = m;
-    __syncthreads();
-    m = sm[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w]);
-  }
-  float l = 0.0f, o[PER];
+  float m = -INFINITY, l = 0.0f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.0f;
-  // Without any key for the row (m = -inf) every part is zeros: nothing to add.
-  for (int p0 = wave; p0 < parts && m > -INFINITY; p0 += WAVES * BATCH) {
+  for (int p0 = wave; p0 < parts; p0 += WAVES * BATCH) {
     float2 ml[BATCH];
     float v[BATCH][PER];
 #pragma unroll
     for (int q = 0; q < BATCH; ++q) {
-      const int64_t s = slot(min(p0 + q * WAVES, parts - 1));
+      const int64_t s = (int64_t)part_slot(join, min(p0 + q * WAVES, parts - 1)) * a.tile_rows + r;
       ml[q] = a.part_ml[s];
 #pragma unroll
       for (int i = 0; i < PER; ++i) v[q][i] = lane < DH ? a.part_o[s * DH + lane * PER + i] : 0.0f;
     }
+    float m_new = m;
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q)
+      if (p0 + q * WAVES < parts) m_new = fmaxf(m_new, ml[q].x);
+    if (m_new == -INFINITY) continue;  // no key for the row so far: nothing but zeros
+    const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= alpha;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) o[i] *= alpha;
 #pragma unroll
     for (int q = 0; q < BATCH; ++q) {
       const bool on = p0 + q * WAVES < parts;
@@ -788,18 +793,28 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention 
     }
   }
   if constexpr (WAVES > 1) {
-    if (lane == 0) so[wave][DH] = l;
+    if (lane == 0) {
+      sm[wave] = m;
+      so[wave][DH] = l;
+    }
     if (lane < DH)
 #pragma unroll
       for (int i = 0; i < PER; ++i) so[wave][lane * PER + i] = o[i];
     __syncthreads();
     if (wave > 0) return;
+    m = sm[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-      l += so[w][DH];
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w]);
+    l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) o[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(sm[w] - m) : 0.0f;
+      l = fmaf(f, so[w][DH], l);
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        if (lane < DH) o[i] += so[w][lane * PER + i];
+        if (lane < DH) o[i] = fmaf(f, so[w][lane * PER + i], o[i]);
     }
   }
   const float inv = m > -INFINITY ? 1.0f / l : 0.0f;

@@ -219,13 +219,14 @@ surge_status surge_op_cache_attention(const surge_kv_cache* cache, int64_t n_row
   a.scale_log2 = scale_log2;
   a.tile_rows = s.tile_rows;
   a.block_shift = s.block_shift;
-  a.by_group = divisor(a.group);
-  a.by_tiles = divisor((int)s.tiles);
-  a.by_heads = divisor(cache->n_kv_heads);
-  a.by_units = divisor(cache->n_seqs * cache->n_kv_heads);
   a.tiles = (int)s.tiles;
   a.units = (int)s.units;
   a.workers = (int)s.workers;
+  a.by_group = divisor(a.group);
+  a.by_tiles = divisor(a.tiles);
+  a.by_heads = divisor(cache->n_kv_heads);
+  a.by_units = divisor(cache->n_seqs * cache->n_kv_heads);
+  a.by_workers = divisor(std::max(a.workers, 1));
   a.least_share = s.least_share;
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)(a.part_o + s.slot_rows() * cache->d_head);
