@@ -239,11 +239,11 @@ struct Block {
 
 // Pages of a wave's next 32 blocks, entry 2 j + t in that lane: tile t of 16
 // keys of block block0 + step j.  -1: no page.
-__device__ __forceinline__ int pages_ahead(const CacheAttention& a, int64_t seq, int block0, int step, int k1) {
+__device__ __forceinline__ int pages_ahead(const CacheAttention& a, int seq, int block0, int step, int k1) {
   const int lane = threadIdx.x & 63;
   const int key = (block0 + step * (lane >> 1)) * 32 + (lane & 1) * 16;
   if (key >= k1) return 0;
-  const int page = a.c.table[seq * a.c.ld_table + (key >> a.c.page_shift)];
+  const int page = a.c.table[(int64_t)seq * a.c.ld_table + (key >> a.c.page_shift)];
   return page >= 0 && page < a.c.n_pages ? page : -1;
 }
 
@@ -301,6 +301,10 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.group;
 
+  // Every key waits for the table: it is asked for first.
+  const int end = (u.k1 + 31) / 32;  // blocks
+  int block = u.k0 / 32 + wave;
+  int pages = block < end ? pages_ahead(a, u.seq, block, WAVES, u.k1) : 0;
   bf16x8 qf[RT][STEPS];
   int limit[RT];
 #pragma unroll
@@ -327,14 +331,9 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
 
   const int64_t head_at = u.kvh * PageLayout<DH>::head_bytes(a.c.page_shift);
   u32x4* const sv = reinterpret_cast<u32x4*>(lds + wave * LDS_WAVE);
-  const int end = (u.k1 + 31) / 32;  // blocks
-  int block = u.k0 / 32 + wave;
-  int pages = 0, entry = 0;
+  int entry = 0;
   Block<DH> next;
-  if (block < end) {
-    pages = pages_ahead(a, u.seq, block, WAVES, u.k1);
-    load_block<DH>(a, head_at, pages, 0, block * 32, u.k1, &next);
-  }
+  if (block < end) load_block<DH>(a, head_at, pages, 0, block * 32, u.k1, &next);
   for (; block < end; block += WAVES) {
     const Block<DH> b = next;
     if (block + WAVES < end) {
@@ -366,14 +365,15 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
     bf16x8 pb[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int seen = min(limit[rt], u.k1) - block * 32 - 4 * quarter;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int i = 0; i < 8; ++i) s[rt][i >> 2][i & 3] *= a.scale_log2;
+      if (some_hidden) {
+        asm volatile("");  // a branch around the comparisons, not a selection by both
+        const int seen = min(limit[rt], u.k1) - block * 32 - 4 * quarter;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[rt][t][r] *= a.scale_log2;
-          if (some_hidden && 16 * t + r >= seen) s[rt][t][r] = -INFINITY;
-        }
+        for (int i = 0; i < 8; ++i)
+          if (16 * (i >> 2) + (i & 3) >= seen) s[rt][i >> 2][i & 3] = -INFINITY;
+      }
       float most = s[rt][0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) most = fmaxf(most, s[rt][i >> 2][i & 3]);
@@ -509,12 +509,6 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   const int least = min(row_limit(a, u, min(row0, u.rows - 1)), u.k1);            // that every row sees
   const int most_keys = min(row_limit(a, u, min(row0 + 31, u.rows - 1)), u.k1);   // that some row sees
 
-  bf16x8 qf[KSTEPS];
-  const int query = over(row, a.by_group);
-  const uint16_t* q = a.q + (int64_t)(u.q_beg + query) * a.ld_q + (u.kvh * G + row - query * G) * DH;
-#pragma unroll
-  for (int kk = 0; kk < KSTEPS; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(q + (kk * 2 + half) * 8);
-
   const int64_t head_at = u.kvh * L::head_bytes(a.c.page_shift);
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
   const int n = (max(u.k1 - u.k0, 0) + KB - 1) / KB;
@@ -526,6 +520,12 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
     return page >= 0 && page < a.c.n_pages ? page : -1;
   };
   int pages = n > 0 ? pages_from(0) : 0;
+  bf16x8 qf[KSTEPS];
+  const int query = over(row, a.by_group);
+  const uint16_t* q = a.q + (int64_t)(u.q_beg + query) * a.ld_q + (u.kvh * G + row - query * G) * DH;
+#pragma unroll
+  for (int kk = 0; kk < KSTEPS; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(q + (kk * 2 + half) * 8);
+
   Quarter<DH> raw_k, raw_v;
   uint32_t raw_ks = 0, raw_vs = 0;
   bool raw_bad = false;
@@ -605,6 +605,7 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
         for (int t = 0; t < T; ++t)
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
       if (key0 + 32 * T > least) {
+        asm volatile("");  // a branch around the comparisons, not a selection by both
         const int seen = limit - key0 - 4 * half;
 #pragma unroll
         for (int r = 0; r < 16 * T; ++r)
@@ -740,26 +741,91 @@ __attribute__((amdgpu_waves_per_eu(PLACES[GROUPS / 2 + 1][DH / 64]))) void tile_
   else one_unit(a, body);
 }
 
-// Joins the parts of a row: WAVES waves take parts w, w + WAVES, ..., BATCH of them
-// loaded together, and are added in order.  A workgroup has ROWS rows of a unit.
-template <int DH, int WAVES, int ROWS, int BATCH>
-__global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention a, int row_groups) {
-  constexpr int PER = DH < 64 ? 1 : DH / 64;
-  static_assert(WAVES == 1 || ROWS == 1, "waves that meet have one row");
-  __shared__ float sm[WAVES], so[WAVES][DH + 1];
-  const int lane = threadIdx.x & 63;
-  const int wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
-  const int index = (int)(blockIdx.x / (unsigned)row_groups);
-  const int r = (int)(blockIdx.x % (unsigned)row_groups) * ROWS +
-                (WAVES == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+// The unit, and of a cut one the workers that have its parts, of a join.
+struct Join {
+  int seq, kvh, row0;
+  int2 workers;
+};
+__device__ __forceinline__ Join join_of(const CacheAttention& a, int index) {
   const int head = over(index, a.by_tiles), tile = index - head * a.tiles;
-  const int seq = over(head, a.by_heads), kvh = head - seq * a.c.n_kv_heads;
-  const int2 join = a.joins[index];  // (of a tile without rows, whatever stands there)
-  const Sequence s = uniform(sequence_of(a, seq));
-  const int row = tile * a.tile_rows + r;
-  if (row >= s.rows || r >= a.tile_rows) return;
-  if (join.x < 0) return;
-  const int parts = join.y - join.x + 1;
+  const int seq = over(head, a.by_heads);
+  return {seq, head - seq * a.c.n_kv_heads, tile * a.tile_rows, a.joins[index]};  // (without rows whatever stands there)
+}
+
+// Joins the parts of units that few workers have: eight rows a wave, 16 bytes a
+// lane, BATCH parts loaded together.
+template <int DH, int BATCH>
+__global__ __launch_bounds__(256) void join_rows_kernel(CacheAttention a, int row_groups) {
+  constexpr int LANES = DH / 4, STEP = 64 / LANES, N = 8 / STEP;  // of a row; rows at a time
+  const int lane = threadIdx.x & 63;
+  const int index = (int)(blockIdx.x / (unsigned)row_groups);
+  const int r0 = (int)(blockIdx.x % (unsigned)row_groups) * 32 + (int)(threadIdx.x >> 6) * 8 + lane / LANES;
+  const Join j = join_of(a, index);
+  const Sequence s = uniform(sequence_of(a, j.seq));
+  const int rows = min(a.tile_rows, s.rows - j.row0);
+  if (rows <= 0 || j.workers.x < 0) return;
+  const int parts = j.workers.y - j.workers.x + 1;
+  float m[N], l[N];
+  f32x4 o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.0f;
+    o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  for (int p0 = 0; p0 < parts; p0 += BATCH) {
+    float2 ml[BATCH][N];
+    f32x4 v[BATCH][N];
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      const int64_t slot = (int64_t)part_slot(j.workers, min(p0 + q, parts - 1)) * a.tile_rows;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int64_t row = slot + min(r0 + i * STEP, rows - 1);
+        ml[q][i] = a.part_ml[row];
+        v[q][i] = *reinterpret_cast<const f32x4*>(a.part_o + row * DH + lane % LANES * 4);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (p0 + q >= parts || ml[q][i].x == -INFINITY) continue;  // (no key for the row in it: zeros)
+        const float top = fmaxf(m[i], ml[q][i].x);
+        const float f = __builtin_amdgcn_exp2f(m[i] - top), g = __builtin_amdgcn_exp2f(ml[q][i].x - top);
+        m[i] = top;
+        l[i] = l[i] * f + ml[q][i].y * g;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) o[i][d] = o[i][d] * f + v[q][i][d] * g;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r = r0 + i * STEP, row = j.row0 + r;
+    if (r >= rows) continue;
+    const float inv = m[i] > -INFINITY ? 1.0f / l[i] : 0.0f;
+    const int query = over(row, a.by_group), G = a.group;
+    uint2 w;
+    w.x = pack_bf16x2(o[i][0] * inv, o[i][1] * inv);
+    w.y = pack_bf16x2(o[i][2] * inv, o[i][3] * inv);
+    *reinterpret_cast<uint2*>(a.out + (int64_t)(s.q_beg + query) * a.ld_out + (j.kvh * G + row - query * G) * DH +
+                              lane % LANES * 4) = w;
+  }
+}
+
+// Joins the parts of a row that many workers have: WAVES waves take parts w, w +
+// WAVES, ..., BATCH of them loaded together, and are added in order.
+template <int DH, int WAVES, int BATCH>
+__global__ __launch_bounds__(64 * WAVES) void join_kernel(CacheAttention a, int rows_each) {
+  constexpr int PER = DH < 64 ? 1 : DH / 64;
+  __shared__ float sm[WAVES], so[WAVES][DH + 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int index = (int)(blockIdx.x / (unsigned)rows_each), r = (int)(blockIdx.x % (unsigned)rows_each);
+  const Join j = join_of(a, index);
+  const Sequence s = uniform(sequence_of(a, j.seq));
+  const int row = j.row0 + r;
+  if (row >= s.rows || r >= a.tile_rows || j.workers.x < 0) return;
+  const int parts = j.workers.y - j.workers.x + 1;
   float m = -INFINITY, l = 0.0f, o[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[i] = 0.0f;
@@ -768,7 +834,7 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention 
     float v[BATCH][PER];
 #pragma unroll
     for (int q = 0; q < BATCH; ++q) {
-      const int64_t s = (int64_t)part_slot(join, min(p0 + q * WAVES, parts - 1)) * a.tile_rows + r;
+      const int64_t s = (int64_t)part_slot(j.workers, min(p0 + q * WAVES, parts - 1)) * a.tile_rows + r;
       ml[q] = a.part_ml[s];
 #pragma unroll
       for (int i = 0; i < PER; ++i) v[q][i] = lane < DH ? a.part_o[s * DH + lane * PER + i] : 0.0f;
@@ -792,34 +858,32 @@ __global__ __launch_bounds__(64 * WAVES * ROWS) void join_kernel(CacheAttention 
       for (int i = 0; i < PER; ++i) o[i] = fmaf(f, on ? v[q][i] : 0.0f, o[i]);
     }
   }
-  if constexpr (WAVES > 1) {
-    if (lane == 0) {
-      sm[wave] = m;
-      so[wave][DH] = l;
-    }
-    if (lane < DH)
+  if (lane == 0) {
+    sm[wave] = m;
+    so[wave][DH] = l;
+  }
+  if (lane < DH)
 #pragma unroll
-      for (int i = 0; i < PER; ++i) so[wave][lane * PER + i] = o[i];
-    __syncthreads();
-    if (wave > 0) return;
-    m = sm[0];
+    for (int i = 0; i < PER; ++i) so[wave][lane * PER + i] = o[i];
+  __syncthreads();
+  if (wave > 0) return;
+  m = sm[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w]);
-    l = 0.0f;
+  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm[w]);
+  l = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) o[i] = 0.0f;
+  for (int i = 0; i < PER; ++i) o[i] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(sm[w] - m) : 0.0f;
-      l = fmaf(f, so[w][DH], l);
+  for (int w = 0; w < WAVES; ++w) {
+    const float f = m > -INFINITY ? __builtin_amdgcn_exp2f(sm[w] - m) : 0.0f;
+    l = fmaf(f, so[w][DH], l);
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (lane < DH) o[i] = fmaf(f, so[w][lane * PER + i], o[i]);
-    }
+    for (int i = 0; i < PER; ++i)
+      if (lane < DH) o[i] = fmaf(f, so[w][lane * PER + i], o[i]);
   }
   const float inv = m > -INFINITY ? 1.0f / l : 0.0f;
   const int query = over(row, a.by_group), G = a.group;
-  uint16_t* out = a.out + (int64_t)(s.q_beg + query) * a.ld_out + (kvh * G + row - query * G) * DH;
+  uint16_t* out = a.out + (int64_t)(s.q_beg + query) * a.ld_out + (j.kvh * G + row - query * G) * DH;
   if constexpr (PER == 2)
     reinterpret_cast<uint32_t*>(out)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
   else if (lane < DH)
@@ -844,12 +908,14 @@ hipError_t launch(const CacheAttention& a, hipStream_t stream) {
   if (a.workers == 0) return hipGetLastError();
   const int rows = (int)std::min<int64_t>(a.tile_rows, (int64_t)a.max_rows * a.group);
   if (a.workers >= 16 * a.units) {
-    hipLaunchKernelGGL((join_kernel<DH, 16, 1, 8>), dim3(a.units * rows), dim3(1024), 0, stream, a, rows);
+    hipLaunchKernelGGL((join_kernel<DH, 16, 8>), dim3(a.units * rows), dim3(1024), 0, stream, a, rows);
   } else if (a.workers >= 4 * a.units) {
-    hipLaunchKernelGGL((join_kernel<DH, 4, 1, 8>), dim3(a.units * rows), dim3(256), 0, stream, a, rows);
+    hipLaunchKernelGGL((join_kernel<DH, 4, 8>), dim3(a.units * rows), dim3(256), 0, stream, a, rows);
+  } else if (a.tile_rows < 64) {
+    hipLaunchKernelGGL((join_kernel<DH, 1, 4>), dim3(a.units * rows), dim3(64), 0, stream, a, rows);
   } else {
-    const int groups = (rows + 3) / 4;
-    hipLaunchKernelGGL((join_kernel<DH, 1, 4, 4>), dim3(a.units * groups), dim3(256), 0, stream, a, groups);
+    const int groups = (rows + 31) / 32;
+    hipLaunchKernelGGL((join_rows_kernel<DH, 3>), dim3(a.units * groups), dim3(256), 0, stream, a, groups);
   }
   return hipGetLastError();
 }
