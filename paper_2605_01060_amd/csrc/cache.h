@@ -32,9 +32,10 @@ struct CacheStore {
   CacheRows r;
   uint16_t *k, *v;  // read by a write, written by a read
   int64_t ld_k, ld_v;
+  int heads_each;  // of a wave: the launch's
 };
-hipError_t launch_cache_write(const CacheStore& a, int d_head, hipStream_t stream);
-hipError_t launch_cache_read(const CacheStore& a, int d_head, hipStream_t stream);
+hipError_t launch_cache_write(CacheStore a, int d_head, hipStream_t stream);
+hipError_t launch_cache_read(CacheStore a, int d_head, hipStream_t stream);
 
 // What a kernel divides a number below 2^31 by d with.
 struct Divisor {

@@ -106,7 +106,7 @@ surge_status store(bool write, const surge_kv_cache* cache, int64_t n_rows, cons
   int dev = 0, n_cus = 0;
   CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
   const CacheStore a = {view_of(cache), rows_of(cache, n_rows, d_cu), const_cast<uint16_t*>(d_k),
-                        const_cast<uint16_t*>(d_v), ld_k, ld_v};
+                        const_cast<uint16_t*>(d_v), ld_k, ld_v, 1};
   HIP_TRY(write ? launch_cache_write(a, cache->d_head, (hipStream_t)hip_stream)
                 : launch_cache_read(a, cache->d_head, (hipStream_t)hip_stream));
   return SURGE_OK;

@@ -16,6 +16,7 @@ namespace surge {
 namespace {
 
 constexpr int ROWS = 16;  // of a wave
+constexpr int64_t FEW_WAVES = 16384;
 
 // Which sequence and position a row is.
 struct RowPlace {
@@ -79,58 +80,92 @@ __device__ __forceinline__ uint8_t* page_of(const CacheView& c, int seq, int pos
   return c.pages + page * c.page_bytes + head * PageLayout<DH>::head_bytes(c.page_shift);
 }
 
+// A wave's rows and heads: ROWS rows from t0 on, of heads head .. last - 1.
+struct Part {
+  int t0, head, last;
+};
+__device__ __forceinline__ bool part_of(const CacheStore& a, Part* p) {
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (a.c.n_kv_heads + a.heads_each - 1) / a.heads_each;
+  const int64_t rows = wave / groups;
+  if (rows * ROWS >= a.r.n_rows) return false;
+  p->t0 = (int)rows * ROWS;
+  p->head = (int)(wave % groups) * a.heads_each;
+  p->last = min(p->head + a.heads_each, a.c.n_kv_heads);
+  return true;
+}
+
 template <int DH>
 __global__ __launch_bounds__(256) void cache_write_kernel(CacheStore a) {
   using L = PageLayout<DH>;
   constexpr int PER = DH / 8;       // lanes of a row
   constexpr int STEP = 64 / PER;    // rows of a wave at a time
   constexpr int N = ROWS / STEP;
-  const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = (int)(wave % a.c.n_kv_heads);
-  const int64_t group = wave / a.c.n_kv_heads;
-  if (group * ROWS >= a.r.n_rows) return;
-  const int t0 = (int)group * ROWS, piece = lane % PER;
-  uint4 x[2][N];
+  const int lane = threadIdx.x & 63, piece = lane % PER;
+  Part part;
+  if (!part_of(a, &part)) return;
+  u32x4 x[2][N];
+  auto load = [&](int head) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int64_t t = min(t0 + n * STEP + lane / PER, a.r.n_rows - 1);
-    x[0][n] = *reinterpret_cast<const uint4*>(a.k + t * a.ld_k + head * DH + piece * 8);
-    x[1][n] = *reinterpret_cast<const uint4*>(a.v + t * a.ld_v + head * DH + piece * 8);
-  }
-  const RowPlace mine = place_of(a.c, a.r, t0, lane % ROWS);
+    for (int n = 0; n < N; ++n) {
+      const int64_t t = min(part.t0 + n * STEP + lane / PER, a.r.n_rows - 1);
+      x[0][n] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.k + t * a.ld_k + head * DH + piece * 8));
+      x[1][n] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.v + t * a.ld_v + head * DH + piece * 8));
+    }
+  };
+  load(part.head);
+  const RowPlace mine = place_of(a.c, a.r, part.t0, lane % ROWS);
+  uint8_t* page[N];  // of head 0
+  int slot[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int from = n * STEP + lane / PER;
     const int seq = __shfl(mine.seq, from), pos = __shfl(mine.pos, from);
-    uint8_t* const page = seq < 0 || pos < 0 ? nullptr : page_of<DH>(a.c, seq, pos, head);
-    const int slot = pos & ((1 << a.c.page_shift) - 1);
+    page[n] = seq < 0 || pos < 0 ? nullptr : page_of<DH>(a.c, seq, pos, 0);
+    slot[n] = pos & ((1 << a.c.page_shift) - 1);
+  }
+  for (int head = part.head; head < part.last; ++head) {
+    uint32_t codes[2][N], bytes[2][N];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const uint32_t xs[4] = {x[w][n].x, x[w][n].y, x[w][n].z, x[w][n].w};
-      // Largest magnitude, as bits (of infinities and NaN the largest).
-      uint32_t most = 0;
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        most = max(most, xs[i] << 16 & 0x7fff0000u);
-        most = max(most, xs[i] & 0x7fff0000u);
+      for (int w = 0; w < 2; ++w) {
+        const uint32_t v[4] = {x[w][n][0], x[w][n][1], x[w][n][2], x[w][n][3]};
+        // Largest magnitude, as bits (of infinities and NaN the largest).
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          most = max(most, v[i] << 16 & 0x7fff0000u);
+          most = max(most, v[i] & 0x7fff0000u);
+        }
+        // Over the four lanes of 32 features.
+        most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0xb1, 0xf, 0xf, true));
+        most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0x4e, 0xf, 0xf, true));
+        // With a = 1.f 2^E: e = E - 2 where 1.f <= 1.75, else E - 1.
+        uint32_t byte = ((max(most, 0x0d800000u) + 0x1fffffu) >> 23) - 2;
+        byte = most >= 0x7f800000u ? NAN_SCALE : min(byte, 252u);
+        const float scale = scale_of(byte);
+        uint32_t c = 0;
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[0]), scale, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[1]), scale, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[2]), scale, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, v[3]), scale, 3);
+        codes[w][n] = c;
+        bytes[w][n] = byte;
       }
-      most = max(most, (uint32_t)__shfl_xor((int)most, 1));
-      most = max(most, (uint32_t)__shfl_xor((int)most, 2));
-      // With a = 1.f 2^E: e = E - 2 where 1.f <= 1.75, else E - 1.
-      uint32_t byte = (max(most, 0x0d800000u) + 0x1fffffu >> 23) - 2;
-      byte = most >= 0x7f800000u ? NAN_SCALE : min(byte, 252u);
-      const float scale = scale_of(byte);
-      uint32_t codes = 0;
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[0]), scale, 0);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[1]), scale, 1);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[2]), scale, 2);
-      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, xs[3]), scale, 3);
-      if (page) {
-        *reinterpret_cast<uint32_t*>(page + L::codes(a.c.page_shift, slot, w) + piece * 4) = codes;
-        if (piece % 4 == 0) page[L::scales(a.c.page_shift, slot, w) + piece / 4] = (uint8_t)byte;
-      }
-    }
+    if (head + 1 < part.last) load(head + 1);
+    const int64_t head_at = head * L::head_bytes(a.c.page_shift);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (page[n])
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          uint8_t* const to = page[n] + head_at;
+          *reinterpret_cast<uint32_t*>(to + L::codes(a.c.page_shift, slot[n], w) + piece * 4) = codes[w][n];
+          if (piece % 4 == 0) to[L::scales(a.c.page_shift, slot[n], w) + piece / 4] = (uint8_t)bytes[w][n];
+        }
   }
 }
 
@@ -138,52 +173,72 @@ template <int DH>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheStore a) {
   using L = PageLayout<DH>;
   constexpr int PER = DH / 8, STEP = 64 / PER, N = ROWS / STEP;
-  const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = (int)(wave % a.c.n_kv_heads);
-  const int64_t group = wave / a.c.n_kv_heads;
-  if (group * ROWS >= a.r.n_rows) return;
-  const int t0 = (int)group * ROWS, piece = lane % PER;
-  const RowPlace mine = place_of(a.c, a.r, t0, lane % ROWS);
-  uint32_t codes[N][2], bytes[N][2];
+  const int lane = threadIdx.x & 63, piece = lane % PER;
+  Part part;
+  if (!part_of(a, &part)) return;
+  const RowPlace mine = place_of(a.c, a.r, part.t0, lane % ROWS);
+  const uint8_t* page[N];  // of head 0; NULL: nothing to read
+  int slot[N];
+  uint32_t without[N];     // the scale byte then: zeros, or NaN where there is no page
   bool row[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int from = n * STEP + lane / PER;
     const int seq = __shfl(mine.seq, from), pos = __shfl(mine.pos, from);
     row[n] = seq >= 0;
-    codes[n][0] = codes[n][1] = 0;
-    bytes[n][0] = bytes[n][1] = pos < 0 ? 1 : NAN_SCALE;  // zeros, or no page
-    if (row[n] && pos >= 0) {
-      const uint8_t* const page = page_of<DH>(a.c, seq, pos, head);
-      const int slot = pos & ((1 << a.c.page_shift) - 1);
-      if (page)
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          codes[n][w] = *reinterpret_cast<const uint32_t*>(page + L::codes(a.c.page_shift, slot, w) + piece * 4);
-          bytes[n][w] = page[L::scales(a.c.page_shift, slot, w) + piece / 4];
-        }
-    }
+    without[n] = pos < 0 ? 1 : NAN_SCALE;
+    page[n] = row[n] && pos >= 0 ? page_of<DH>(a.c, seq, pos, 0) : nullptr;
+    slot[n] = pos & ((1 << a.c.page_shift) - 1);
   }
+  uint32_t codes[2][N], bytes[2][N];
+  auto load = [&](int head) {
+    const int64_t head_at = head * L::head_bytes(a.c.page_shift);
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int64_t t = t0 + n * STEP + lane / PER;
-    if (!row[n]) continue;
-    *reinterpret_cast<u32x4*>(a.k + t * a.ld_k + head * DH + piece * 8) =
-        __builtin_bit_cast(u32x4, decode8(codes[n][0], scale_of(bytes[n][0])));
-    *reinterpret_cast<u32x4*>(a.v + t * a.ld_v + head * DH + piece * 8) =
-        __builtin_bit_cast(u32x4, decode8(codes[n][1], scale_of(bytes[n][1])));
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        codes[w][n] = 0;
+        bytes[w][n] = without[n];
+        if (page[n]) {
+          const uint8_t* const from = page[n] + head_at;
+          codes[w][n] = *reinterpret_cast<const uint32_t*>(from + L::codes(a.c.page_shift, slot[n], w) + piece * 4);
+          bytes[w][n] = from[L::scales(a.c.page_shift, slot[n], w) + piece / 4];
+        }
+      }
+  };
+  load(part.head);
+  for (int head = part.head; head < part.last; ++head) {
+    u32x4 x[2][N];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) x[w][n] = __builtin_bit_cast(u32x4, decode8(codes[w][n], scale_of(bytes[w][n])));
+    if (head + 1 < part.last) load(head + 1);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int64_t t = part.t0 + n * STEP + lane / PER;
+      if (!row[n]) continue;
+      __builtin_nontemporal_store(x[0][n], reinterpret_cast<u32x4*>(a.k + t * a.ld_k + head * DH + piece * 8));
+      __builtin_nontemporal_store(x[1][n], reinterpret_cast<u32x4*>(a.v + t * a.ld_v + head * DH + piece * 8));
+    }
   }
 }
 
-unsigned blocks(const CacheStore& a) {
+// Heads of a wave: one in small calls, which need the waves, four in large ones,
+// whose waves find their rows' places once for them.
+int heads_each(const CacheStore& a) {
   const int64_t waves = ((int64_t)a.r.n_rows + ROWS - 1) / ROWS * a.c.n_kv_heads;
-  return (unsigned)((waves + 3) / 4);
+  return waves > FEW_WAVES ? 4 : 1;
+}
+unsigned blocks(const CacheStore& a) {
+  const int64_t groups = (a.c.n_kv_heads + a.heads_each - 1) / a.heads_each;
+  return (unsigned)((((int64_t)a.r.n_rows + ROWS - 1) / ROWS * groups + 3) / 4);
 }
 
 }  // namespace
 
-hipError_t launch_cache_write(const CacheStore& a, int d_head, hipStream_t stream) {
+hipError_t launch_cache_write(CacheStore a, int d_head, hipStream_t stream) {
+  a.heads_each = heads_each(a);
   const dim3 grid(blocks(a));
   if (d_head == 32) hipLaunchKernelGGL(cache_write_kernel<32>, grid, dim3(256), 0, stream, a);
   if (d_head == 64) hipLaunchKernelGGL(cache_write_kernel<64>, grid, dim3(256), 0, stream, a);
@@ -191,7 +246,8 @@ hipError_t launch_cache_write(const CacheStore& a, int d_head, hipStream_t strea
   return hipGetLastError();
 }
 
-hipError_t launch_cache_read(const CacheStore& a, int d_head, hipStream_t stream) {
+hipError_t launch_cache_read(CacheStore a, int d_head, hipStream_t stream) {
+  a.heads_each = heads_each(a);
   const dim3 grid(blocks(a));
   if (d_head == 32) hipLaunchKernelGGL(cache_read_kernel<32>, grid, dim3(256), 0, stream, a);
   if (d_head == 64) hipLaunchKernelGGL(cache_read_kernel<64>, grid, dim3(256), 0, stream, a);
