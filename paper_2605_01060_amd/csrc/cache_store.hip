@@ -85,7 +85,8 @@ struct Part {
   int t0, head, last;
 };
 __device__ __forceinline__ bool part_of(const CacheStore& a, Part* p) {
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t block = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  const int64_t wave = block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = (a.c.n_kv_heads + a.heads_each - 1) / a.heads_each;
   const int64_t rows = wave / groups;
   if (rows * ROWS >= a.r.n_rows) return false;
@@ -232,7 +233,7 @@ int heads_each(const CacheStore& a) {
 }
 unsigned blocks(const CacheStore& a) {
   const int64_t groups = (a.c.n_kv_heads + a.heads_each - 1) / a.heads_each;
-  return (unsigned)((((int64_t)a.r.n_rows + ROWS - 1) / ROWS * groups + 3) / 4);
+  return (unsigned)((((int64_t)a.r.n_rows + ROWS - 1) / ROWS * groups + 31) / 32 * 8);
 }
 
 }  // namespace
