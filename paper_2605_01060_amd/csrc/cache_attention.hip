@@ -17,7 +17,7 @@ namespace surge {
 namespace {
 
 // Workgroups of a kernel on a CU, by its class (few rows: 16, 32; tiles of 64, 128) and d_head, that registers and LDS allow.
-constexpr int PLACES[4][3] = {{5, 4, 3}, {4, 3, 2}, {4, 3, 2}, {4, 3, 2}};
+constexpr int PLACES[4][3] = {{7, 4, 3}, {5, 3, 2}, {5, 4, 2}, {5, 3, 2}};
 
 // The 16 bytes of codes (d_head 128; 8 or 4 for smaller heads) of a quarter of
 // a key or value.
@@ -70,6 +70,14 @@ __device__ __forceinline__ Sequence sequence_of(const CacheAttention& a, int seq
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ Sequence uniform(const Sequence& s) {
   return {uniform(s.q_beg), uniform(s.rows), uniform(s.first), uniform(s.length)};
+}
+
+// The lane's number, made anew where it is asked for: what a unit's code makes of it
+// is not kept in registers from unit to unit (up to 50 of them).
+__device__ __forceinline__ int own_lane() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
 }
 
 // A unit of work: a tile of rows of one (sequence, key head), with all of the keys
@@ -136,28 +144,24 @@ __device__ __forceinline__ void one_unit(const CacheAttention& a, Body body) {
 }
 
 // The workgroup's equal share of all units' blocks of keys, in the order of
-// sequence, key head, tile: it starts and ends anywhere, and the parts of a unit
-// that is cut are joined afterwards.  Workgroups of one XCD have shares next to each
-// other, whose units share keys.
+// sequence, tile, key head: it starts and ends anywhere, and the parts of a unit that
+// is cut are joined afterwards.  Workgroups of one XCD have shares next to each other,
+// of a sequence's keys.
 template <class Body>
 __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body) {
-  __shared__ int s_before[256], s_wave[4];  // blocks before a thread's sequences
+  __shared__ int s_before[256], s_wave[4];  // blocks before a thread's (sequence, tile) pairs
   __shared__ Sequence s_first[256];         // its first sequence
   const int worker = (int)(blockIdx.x % 8) * (a.workers / 8) + (int)(blockIdx.x / 8);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (a.c.n_seqs + 255) >> 8;
-  auto blocks_of_head = [&](const Sequence& s) {
-    int n = 0;
-    for (int t = 0; t < a.tiles; ++t) n += blocks_of(a, s, t);
-    return n;
-  };
+  const int pairs = a.c.n_seqs * a.tiles, per = (pairs + 255) >> 8, heads = a.c.n_kv_heads;
   int mine = 0;
   for (int i = 0; i < per; ++i) {
-    const int seq = (int)threadIdx.x * per + i;
-    if (seq >= a.c.n_seqs) break;
+    const int pair = (int)threadIdx.x * per + i;
+    if (pair >= pairs) break;
+    const int seq = over(pair, a.by_tiles);
     const Sequence s = sequence_of(a, seq);
     if (i == 0) s_first[threadIdx.x] = s;
-    mine += blocks_of_head(s) * a.c.n_kv_heads;
+    mine += blocks_of(a, s, pair - seq * a.tiles) * heads;
   }
   const int upto = scan64(mine);
   if (lane == 63) s_wave[wave] = upto;
@@ -175,41 +179,38 @@ __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body)
   int at = worker * share;
   const int end = min(at + share, total);
   if (at >= end) return;
-  // The last thread whose sequences start at or before `at`, then the sequence,
-  // its key head and tile.
+  // The last thread whose pairs start at or before `at`, then the pair.
   int thread = -1;
 #pragma unroll
   for (int i = 0; i < 4; ++i) thread += __popcll(__ballot(s_before[i * 64 + lane] <= at));
   thread = uniform(thread);
-  int seq = thread * per, start = uniform(s_before[thread]);
-  for (bool first = true; at < end; ++seq, first = false) {
-    const Sequence s = uniform(first ? s_first[thread] : sequence_of(a, seq));
-    const int n_head = uniform(blocks_of_head(s));
-    if (at >= start + n_head * a.c.n_kv_heads) {
-      start += n_head * a.c.n_kv_heads;
+  int start = uniform(s_before[thread]);
+  Sequence s = uniform(s_first[thread]);
+  for (int pair = thread * per, of = -1; at < end; ++pair) {
+    const int seq = over(pair, a.by_tiles), tile = pair - seq * a.tiles;
+    if (of >= 0 && of != seq) s = uniform(sequence_of(a, seq));
+    of = seq;
+    const int n = blocks_of(a, s, tile);
+    if (at >= start + n * heads) {
+      start += n * heads;
       continue;
     }
-    const int past = a.c.n_kv_heads == 1 ? 0 : (at - start) / n_head;
-    start += past * n_head;
-    for (int kvh = past; kvh < a.c.n_kv_heads && at < end; ++kvh)
-      for (int tile = 0; tile < a.tiles && at < end; ++tile) {
-        const int n = blocks_of(a, s, tile);
-        if (at < start + n) {
-          Unit u = unit_of(a, s, seq, kvh, tile);
-          const int from = at - start, to = min(n, end - start);
-          u.whole = from == 0 && to == n;
-          u.k0 = from << a.block_shift;
-          u.k1 = min(to << a.block_shift, u.limit);
-          u.slot = 2 * worker + (from == 0);
-          body(u);
-          // Who has a unit's last part knows where it started.
-          if (to == n && threadIdx.x == 0)
-            a.joins[(seq * a.c.n_kv_heads + kvh) * a.tiles + tile] = make_int2(u.whole ? -1 : start / share, worker);
-          at = start + to;
-          if (at < end) __syncthreads();  // LDS is read out
-        }
-        start += n;
-      }
+    const int past = (at - start) / n;
+    start += past * n;
+    for (int kvh = past; kvh < heads && at < end; ++kvh, start += n) {
+      Unit u = unit_of(a, s, seq, kvh, tile);
+      const int from = at - start, to = min(n, end - start);
+      u.whole = from == 0 && to == n;
+      u.k0 = from << a.block_shift;
+      u.k1 = min(to << a.block_shift, u.limit);
+      u.slot = 2 * worker + (from == 0);
+      body(u);
+      // Who has a unit's last part knows where it started.
+      if (to == n && threadIdx.x == 0)
+        a.joins[pair * heads + kvh] = make_int2(u.whole ? -1 : start / share, worker);
+      at = start + to;
+      if (at < end) __syncthreads();  // LDS is read out
+    }
   }
 }
 
@@ -249,9 +250,9 @@ __device__ __forceinline__ int pages_ahead(const CacheAttention& a, int seq, int
 
 template <int DH>
 __device__ __forceinline__ void load_block(const CacheAttention& a, int64_t head_at, int pages, int entry,
-                                           int key0, int k1, Block<DH>* b) {
+                                           int key0, int lane, Block<DH>* b) {
   using L = PageLayout<DH>;
-  const int lane = threadIdx.x & 63, quarter = lane >> 4;
+  const int quarter = lane >> 4;
   const int shift = a.c.page_shift, mask = (1 << shift) - 1;
   b->bad = 0;
 #pragma unroll
@@ -297,7 +298,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
   constexpr int LDS_WAVE = (32 * DH * 2 > 16 * STRIDE * 4 ? 32 * DH * 2 : 16 * STRIDE * 4);
   __shared__ __attribute__((aligned(256))) uint8_t lds[RT * WAVES * LDS_WAVE];
   __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
-  const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
+  const int lane = own_lane(), col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.group;
 
@@ -333,7 +334,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
   u32x4* const sv = reinterpret_cast<u32x4*>(lds + wave * LDS_WAVE);
   int entry = 0;
   Block<DH> next;
-  if (block < end) load_block<DH>(a, head_at, pages, 0, block * 32, u.k1, &next);
+  if (block < end) load_block<DH>(a, head_at, pages, 0, block * 32, lane, &next);
   for (; block < end; block += WAVES) {
     const Block<DH> b = next;
     if (block + WAVES < end) {
@@ -342,7 +343,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
         entry = 0;
         pages = pages_ahead(a, u.seq, block + WAVES, WAVES, u.k1);
       }
-      load_block<DH>(a, head_at, pages, entry, (block + WAVES) * 32, u.k1, &next);
+      load_block<DH>(a, head_at, pages, entry, (block + WAVES) * 32, lane, &next);
     }
     f32x4 s[RT][2];
 #pragma unroll
@@ -440,7 +441,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
           f32x4{o[rt][f][0] * alpha, o[rt][f][1] * alpha, o[rt][f][2] * alpha, o[rt][f][3] * alpha};
     __syncthreads();
     // Sixteen threads a row, four features each at a time.
-    const int r = threadIdx.x >> 4, row = u.row0 + rt * 16 + r;
+    const int r = wave * 4 + quarter, row = u.row0 + rt * 16 + r;
     if (row < u.rows) {
       float ml = s_m[0][rt * 16 + r], l = 0.0f;
 #pragma unroll
@@ -450,7 +451,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
         l = fmaf(__builtin_amdgcn_exp2f(s_m[w][rt * 16 + r] - ml), s_l[w][rt * 16 + r], l);
       const bool seen = min(row_limit(a, u, row), u.k1) > u.k0;
       const float inv = seen ? 1.0f / l : 0.0f;
-      for (int d = (threadIdx.x & 15) * 4; d < DH; d += 64) {
+      for (int d = col * 4; d < DH; d += 64) {
         f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
@@ -498,7 +499,7 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   constexpr int KSTEPS = DH / 16, DT = DH / 32, CPR = DH / 8, STEPS = DH / 32, KB = 64, T = GROUPS / 2;  // T: 32-key tiles of a wave
   constexpr uint32_t ROW = DH * 2, BUF = KB * ROW;
   __shared__ __attribute__((aligned(256))) u32x4 sKV[4 * BUF / 16];  // K blocks by parity, then V blocks
-  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int lane = own_lane(), col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.group;
   const int rows_of = wave % GROUPS, key_part = wave / GROUPS;
@@ -747,9 +748,8 @@ struct Join {
   int2 workers;
 };
 __device__ __forceinline__ Join join_of(const CacheAttention& a, int index) {
-  const int head = over(index, a.by_tiles), tile = index - head * a.tiles;
-  const int seq = over(head, a.by_heads);
-  return {seq, head - seq * a.c.n_kv_heads, tile * a.tile_rows, a.joins[index]};  // (without rows whatever stands there)
+  const int pair = over(index, a.by_heads), seq = over(pair, a.by_tiles);
+  return {seq, index - pair * a.c.n_kv_heads, (pair - seq * a.tiles) * a.tile_rows, a.joins[index]};  // (without rows whatever stands there)
 }
 
 // Joins the parts of units that few workers have: eight rows a wave, 16 bytes a
@@ -941,7 +941,7 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
   const int64_t most = ((max_length - 1) >> s.block_shift) + 1;  // blocks of a unit
   s.least_share = cls >= 2 ? 8 : 2;
   s.workers = 0;
-  if (most > (cls >= 2 ? 32 : 8) && n_seqs <= 2048 && s.units * most < INT32_MAX && s.units <= 2 * workers)
+  if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < INT32_MAX && s.units <= 2 * workers)
     s.workers = workers;
   return s;
 }
