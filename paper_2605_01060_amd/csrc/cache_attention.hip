@@ -362,6 +362,24 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
             __builtin_bit_cast(u32x4, decode8(b.v[t].w[kk], v_scale));
       }
     }
+    // V^T of feature tile f: keys 4 quarter .. + 3 and 16 further on, as the
+    // scores' registers have them.  Half of the tiles are asked for before the
+    // softmax and the others before the first half's products.
+    auto v_fragment = [&](int f) {
+      bf16x4 v[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int key = 16 * t + 4 * quarter + (col >> 2);
+        const uint32_t at = lds_address(sv) + v_slot<CPR>(key, 2 * f + (col >> 1 & 1)) * 16 + (col & 1) * 8;
+        v[t] = __builtin_bit_cast(
+            bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+      }
+      return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    bf16x8 vf[FT];
+#pragma unroll
+    for (int f = 0; f < FT / 2; ++f) vf[f] = v_fragment(f);
+    __builtin_amdgcn_sched_barrier(0);
     const bool some_hidden = block * 32 + 32 > least || block * 32 + 32 > u.k1;
     bf16x8 pb[RT];
 #pragma unroll
@@ -398,23 +416,14 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
         pb[rt][i] = (__bf16)p;
       }
     }
-    // V^T of feature tile f: keys 4 quarter .. + 3 and 16 further on, as the
-    // scores' registers have them.
 #pragma unroll
-    for (int f = 0; f < FT; ++f) {
-      bf16x4 v[2];
+    for (int f = FT / 2; f < FT; ++f) vf[f] = v_fragment(f);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int key = 16 * t + 4 * quarter + (col >> 2);
-        const uint32_t at = lds_address(sv) + v_slot<CPR>(key, 2 * f + (col >> 1 & 1)) * 16 + (col & 1) * 8;
-        v[t] = __builtin_bit_cast(
-            bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
-      }
-      const bf16x8 vf = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    for (int f = 0; f < FT; ++f)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
-        o[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[rt], o[rt][f], 0, 0, 0);
-    }
+        o[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[f], pb[rt], o[rt][f], 0, 0, 0);
   }
 
   // The waves' parts are joined.  Register r of tile f: feature 16 f + 4
