@@ -143,16 +143,43 @@ __device__ __forceinline__ void one_unit(const CacheAttention& a, Body body) {
   if (tile * a.tile_rows < s.rows) body(unit_of(a, s, seq, rest - seq * a.c.n_kv_heads, tile));
 }
 
-// The workgroup's equal share of all units' blocks of keys, in the order of
-// sequence, tile, key head: it starts and ends anywhere, and the parts of a unit that
-// is cut are joined afterwards.  Workgroups of one XCD have shares next to each other,
-// of a sequence's keys.
+// Sums of a value over the workgroup's threads before this one, and over all.
+__device__ __forceinline__ int2 sums_before(int v, int* s_wave) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int upto = scan64(v);
+  if (lane == 63) s_wave[wave] = upto;
+  __syncthreads();
+  int before = upto - v, total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += s_wave[w];
+    total += s_wave[w];
+  }
+  return make_int2(before, uniform(total));
+}
+
+// The last of 256 increasing numbers that is at most `at`.
+__device__ __forceinline__ int last_upto(const int* before, int at) {
+  int n = -1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) n += __popcll(__ballot(before[i * 64 + (threadIdx.x & 63)] <= at));
+  return uniform(n);
+}
+
+// The workgroup's part of all units' blocks of keys.  Workgroups of one XCD have
+// parts next to each other, of a sequence's keys, in the order of sequence, tile,
+// key head.
+//
+// Few units are cut into equal parts each, as many as keep them to the share of a
+// worker, so that no worker has two (16 sequences, 5 queries, 3001 keys, 16 / 4 x
+// 128: a unit's start and end take 5 us, a block 1.6).  Of more units each worker
+// has an equal share, which starts and ends anywhere.  The parts of a unit that is
+// cut are joined afterwards; who has the last one knows where they started.
 template <class Body>
 __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body) {
-  __shared__ int s_before[256], s_wave[4];  // blocks before a thread's (sequence, tile) pairs
-  __shared__ Sequence s_first[256];         // its first sequence
+  __shared__ int s_before[256], s_wave[3][4];  // what lies before a thread's (sequence, tile) pairs
+  __shared__ Sequence s_first[256];            // its first sequence
   const int worker = (int)(blockIdx.x % 8) * (a.workers / 8) + (int)(blockIdx.x / 8);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pairs = a.c.n_seqs * a.tiles, per = (pairs + 255) >> 8, heads = a.c.n_kv_heads;
   int mine = 0;
   for (int i = 0; i < per; ++i) {
@@ -163,27 +190,43 @@ __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body)
     if (i == 0) s_first[threadIdx.x] = s;
     mine += blocks_of(a, s, pair - seq * a.tiles) * heads;
   }
-  const int upto = scan64(mine);
-  if (lane == 63) s_wave[wave] = upto;
-  __syncthreads();
-  int before = upto - mine, total = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += s_wave[w];
-    total += s_wave[w];
+  const int2 blocks = sums_before(mine, s_wave[0]);
+  const int total = blocks.y;
+  if (a.units <= a.workers / 4) {  // (a pair a thread then)
+    // The least share, if its parts are no more than the workers, else one that is
+    // sure to be.
+    const int n_mine = over(mine, a.by_heads);
+    int share = max(over(total + a.workers - 1, a.by_workers), a.least_share);
+    int2 parts = sums_before((n_mine + share - 1) / share * heads, s_wave[1]);
+    if (parts.y > a.workers) {
+      share = max((total + a.workers - a.units - 1) / (a.workers - a.units), a.least_share);
+      parts = sums_before((n_mine + share - 1) / share * heads, s_wave[2]);
+    }
+    s_before[threadIdx.x] = parts.x;
+    __syncthreads();
+    if (worker >= parts.y) return;
+    const int pair = last_upto(s_before, worker);
+    const Sequence s = uniform(s_first[pair]);
+    const int seq = over(pair, a.by_tiles), tile = pair - seq * a.tiles;
+    const int n = blocks_of(a, s, tile), cuts = (n + share - 1) / share, size = (n + cuts - 1) / cuts;
+    const int past = worker - uniform(s_before[pair]), kvh = past / cuts, part = past - kvh * cuts;
+    Unit u = unit_of(a, s, seq, kvh, tile);
+    u.whole = cuts == 1;
+    u.k0 = part * size << a.block_shift;
+    u.k1 = min((part + 1) * size << a.block_shift, u.limit);
+    u.slot = 2 * worker + (part == 0);
+    if (part == cuts - 1 && threadIdx.x == 0)
+      a.joins[pair * heads + kvh] = make_int2(u.whole ? -1 : worker - part, worker);
+    body(u);
+    return;
   }
-  s_before[threadIdx.x] = before;
+  s_before[threadIdx.x] = blocks.x;
   __syncthreads();
-  total = uniform(total);
   const int share = max(over(total + a.workers - 1, a.by_workers), a.least_share);
   int at = worker * share;
   const int end = min(at + share, total);
   if (at >= end) return;
-  // The last thread whose pairs start at or before `at`, then the pair.
-  int thread = -1;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) thread += __popcll(__ballot(s_before[i * 64 + lane] <= at));
-  thread = uniform(thread);
+  const int thread = last_upto(s_before, at);
   int start = uniform(s_before[thread]);
   Sequence s = uniform(s_first[thread]);
   for (int pair = thread * per, of = -1; at < end; ++pair) {
@@ -205,7 +248,6 @@ __device__ __forceinline__ void shared_units(const CacheAttention& a, Body body)
       u.k1 = min(to << a.block_shift, u.limit);
       u.slot = 2 * worker + (from == 0);
       body(u);
-      // Who has a unit's last part knows where it started.
       if (to == n && threadIdx.x == 0)
         a.joins[pair * heads + kvh] = make_int2(u.whole ? -1 : start / share, worker);
       at = start + to;
