@@ -17,7 +17,7 @@ namespace surge {
 namespace {
 
 // Workgroups of a kernel on a CU, by its class (few rows: 16, 32; tiles of 64, 128) and d_head, that registers and LDS allow.
-constexpr int PLACES[4][3] = {{7, 4, 3}, {5, 3, 2}, {5, 4, 2}, {5, 3, 2}};
+constexpr int PLACES[4][3] = {{7, 4, 3}, {5, 3, 2}, {5, 4, 2}, {4, 3, 2}};
 
 // The 16 bytes of codes (d_head 128; 8 or 4 for smaller heads) of a quarter of
 // a key or value.
@@ -787,7 +787,7 @@ __attribute__((amdgpu_waves_per_eu(PLACES[RT / 2][DH / 64]))) void few_rows_kern
 
 template <int DH, int GROUPS, bool SHARED>
 __global__ __launch_bounds__(256)
-__attribute__((amdgpu_waves_per_eu(PLACES[GROUPS / 2 + 1][DH / 64]))) void tile_kernel(CacheAttention a) {
+__attribute__((amdgpu_waves_per_eu(SHARED ? PLACES[GROUPS / 2 + 1][DH / 64] : 2))) void tile_kernel(CacheAttention a) {
   auto body = [&](const Unit& u) { tile_unit<DH, GROUPS>(a, u); };
   if constexpr (SHARED) shared_units(a, body);
   else one_unit(a, body);
