@@ -992,7 +992,7 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
   const int64_t most = ((max_length - 1) >> s.block_shift) + 1;  // blocks of a unit
   s.least_share = cls >= 2 ? 8 : 2;
   s.workers = 0;
-  if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < INT32_MAX && s.units <= 2 * workers)
+  if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) && s.units <= 2 * workers)
     s.workers = workers;
   return s;
 }

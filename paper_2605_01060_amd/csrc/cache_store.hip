@@ -24,8 +24,9 @@ struct RowPlace {
 };
 
 // The places of rows t0 + r (r < ROWS, one per lane).  cu is searched by 64
-// lanes at a time, then the boundaries from there on are walked in registers.
-// Offsets that decrease give places within bounds, whatever they are.
+// lanes at a time (not at all where a wave holds it), then the boundaries from there
+// on are walked in registers.  Offsets that decrease give places within bounds,
+// whatever they are.
 __device__ __forceinline__ RowPlace place_of(const CacheView& c, const CacheRows& rows, int t0, int r) {
   RowPlace at = {-1, 0, 0};
   const int t = t0 + r;
@@ -38,21 +39,24 @@ __device__ __forceinline__ RowPlace place_of(const CacheView& c, const CacheRows
     return at;
   }
   const int lane = threadIdx.x & 63;
-  int lo = 0, hi = c.n_seqs;  // the last i with cu[i] <= t0 is in [lo, hi)
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 63) / 64;
-    const int i = lo + lane * step;
-    const int n = __popcll(__ballot(i < hi && rows.cu[min(i, c.n_seqs)] <= t0));
-    if (n > 0) lo += (n - 1) * step;
-    hi = min(lo + step, hi);
-  }
+  int lo = 0;
+  if (c.n_seqs > 64)
+    for (int hi = c.n_seqs; hi - lo > 1;) {  // the last i with cu[i] <= t0 is in [lo, hi)
+      const int step = (hi - lo + 63) / 64;
+      const int i = lo + lane * step;
+      const int n = __popcll(__ballot(i < hi && rows.cu[min(i, c.n_seqs)] <= t0));
+      if (n > 0) lo += (n - 1) * step;
+      hi = min(lo + step, hi);
+    }
   int seq = lo, end = 0;
   bool found = false;
   const int first = rows.cu[lo];
   for (int base = lo + 1; base <= c.n_seqs; base += 64) {
     const int bounds = rows.cu[min(base + lane, c.n_seqs)];
     const int n = min(64, c.n_seqs - base + 1);
-    for (int e = 0; e < n; ++e) {
+    const int before = __popcll(__ballot(lane < n && bounds <= t0));
+    if (before > 0) seq = base + before - 1;
+    for (int e = before; e < n; ++e) {
       const int bound = __builtin_amdgcn_readlane(bounds, e);
       if (!found && t >= bound) seq = base + e;
       if (!found && t < bound) {

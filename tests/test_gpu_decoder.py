@@ -374,6 +374,29 @@ def test_attention_over_long_sequences(lengths, rows, page, heads, hk, dh, causa
     assert torch.equal(out, again)  # no order of arrival in the result
 
 
+# Calls whose units are shared out with cuts anywhere, a thread's (sequence, tile)
+# pairs one or several, and calls of a unit a workgroup; lengths that differ, some
+# sequences without rows or keys.
+BATCHES = [(60, 1, 3000, 64, 32, 8, 128), (300, 1, 2500, 32, 4, 1, 64), (700, 2, 1400, 16, 2, 1, 32),
+           (40, 7, 2200, 64, 12, 4, 128), (90, 9, 1500, 32, 6, 2, 64), (7, 350, 3000, 64, 8, 4, 128),
+           (30, 12, 2600, 64, 16, 4, 64), (500, 1, 1300, 128, 8, 8, 32), (6, 260, 2500, 16, 9, 9, 32)]
+
+
+@pytest.mark.parametrize("seqs,rows,length,page,heads,hk,dh", BATCHES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_batches(seqs, rows, length, page, heads, hk, dh, causal):
+    torch = torch_cuda()
+    rng = np.random.default_rng(seqs)
+    lengths = rng.integers(1, length, seqs)
+    lengths[rng.random(seqs) < 0.1] = 0
+    lengths[seqs // 2], lengths[-1] = length, 0
+    counts = rng.integers(1, rows + 1, seqs)
+    counts[rng.random(seqs) < 0.1] = 0
+    counts[seqs // 2] = rows
+    c = Cache(lengths, page, hk, dh, seqs).fill(2)
+    check(c, [int(r) for r in counts], heads, causal, 3)
+
+
 def test_attention_of_prompts_without_a_cache_before():
     """Rows for every position of sequences, one tile and more."""
     lengths = [130, 64, 1, 257, 640]
