@@ -640,10 +640,12 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   }
   for (int i = 0; i < n; ++i) {
     __syncthreads();  // the block is there, the other one read out
-    if (i + 1 < n) {
-      decode(i + 1);
-      if (i + 2 < n) load(i + 2);
-    }
+    auto next_block = [&] {
+      if (i + 1 < n) {
+        decode(i + 1);
+        if (i + 2 < n) load(i + 2);
+      }
+    };
     const int key0 = u.k0 + i * KB + key_part * 32;
     if (active && key0 < most_keys) {
       f32x16 s[T];
@@ -651,11 +653,15 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
       for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+      // Ahead of the waves of the SIMD that are at their exponentials.
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int kk = 0; kk < KSTEPS; ++kk)
 #pragma unroll
         for (int t = 0; t < T; ++t)
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
+      __builtin_amdgcn_s_setprio(0);
+      next_block();
       if (key0 + 32 * T > least) {
         asm volatile("");  // a branch around the comparisons, not a selection by both
         const int seen = limit - key0 - 4 * half;
@@ -700,6 +706,8 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
         for (int dt = 0; dt < DT; ++dt)
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(c, dt), pb, o[dt], 0, 0, 0);
       }
+    } else {
+      next_block();
     }
     const uint32_t other = i & 1 ? 0u - BUF : BUF;
     ka += other;
