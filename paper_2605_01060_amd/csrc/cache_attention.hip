@@ -320,15 +320,16 @@ __device__ __forceinline__ void scales_of(uint32_t ks, uint32_t vs, bool there, 
   *v = scale_of(!there || nan ? 1u : vs);
 }
 
-// Position of 16-byte chunk `chunk` of row `key` of V in LDS, rows of CPR
-// chunks: the transposing reads take 32 bytes of eight consecutive rows at a
-// time and the writes one chunk of sixteen, neither with a bank conflict at
-// d_head 64 and 128 (two-way in a part of the writes at 32).
+// Position of 16-byte chunk `chunk` of row `key` of V in LDS, rows of CPR chunks.
+// The transposing reads take 32 bytes of eight consecutive rows at a time, which
+// lie on different banks of the 64; a write takes one chunk of eight rows at a time,
+// which lie on different ones of the 32 that it has (of 64 they did before: 8 cycles
+// more for each write, 1 % of the time).
 template <int CPR>
 __device__ __forceinline__ uint32_t v_slot(int key, int chunk) {
-  if constexpr (CPR == 16) return key * 16 + (chunk ^ ((key & 7) << 1 | (key >> 3 & 1)));
-  if constexpr (CPR == 8) return key * 8 + (chunk ^ ((key >> 1 & 3) << 1 | (key >> 3 & 1)));
-  return key * 4 + (chunk ^ (key >> 2 & 1) * 3);
+  if constexpr (CPR == 16) return key * 16 + (chunk ^ ((key & 7) << 1 | (key >> 2 & 1)));
+  if constexpr (CPR == 8) return key * 8 + (chunk ^ (key & 7));
+  return key * 4 + (chunk ^ (key >> 1 & 3));
 }
 
 // Few rows: RT tiles of 16 against blocks of 32 keys, each wave of four with
@@ -530,13 +531,16 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
 // with 2 against half of it, and the halves are joined in the end.
 //
 // Chunk c of row r is stored at c ^ f(r), so that neither the reads of K (a chunk
-// of 32 rows), the transposing reads of V (64 bytes of four consecutive rows) nor,
-// at d_head 128, the writes (a chunk of 16 rows) have bank conflicts.
+// of 16 of 32 rows at a time, on 64 banks), the transposing reads of V (64 bytes of
+// four consecutive rows) nor the writes (a chunk of eight consecutive rows, on 32
+// banks) have bank conflicts.  With r3 .. r0 the bits of r, f's are r1 ^ r3, r0, r1,
+// r2 for rows of 16 chunks, r1, r2, r0 ^ r3 for 8 and r2, r1 ^ r3 for 4.
 template <int CPR>
 __device__ __forceinline__ uint32_t kv_position(int row, int chunk) {
-  if constexpr (CPR == 16) return row * 16 + (chunk ^ ((row & 3) << 2 | (row >> 2 & 3)));
-  if constexpr (CPR == 8) return row * 8 + (chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3)));
-  return swz<4>(row, chunk);
+  if constexpr (CPR == 16)
+    return row * 16 + (chunk ^ (((row >> 1 ^ row >> 3) & 1) << 3 | (row & 1) << 2 | (row & 2) | (row >> 2 & 1)));
+  if constexpr (CPR == 8) return row * 8 + (chunk ^ ((row & 2) << 1 | (row >> 1 & 2) | ((row ^ row >> 3) & 1)));
+  return row * 4 + (chunk ^ ((row >> 1 & 3) ^ (row >> 3 & 1)));
 }
 
 __device__ __forceinline__ float over_halves(float v, float (*op)(float, float)) {
@@ -610,7 +614,7 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
   const int tr_feat = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   uint32_t ka = lds + key_part * 32 * ROW + kv_position<CPR>(col, half) * 16u;
   uint32_t va = lds + key_part * 32 * ROW + 2 * BUF + kv_position<CPR>(tr_key, tr_feat >> 3) * 16u + (tr_feat & 7) * 2u;
-  constexpr uint32_t H_SWZ = CPR == 4 ? 16 : 32;  // of 8 keys further on
+  constexpr uint32_t H_SWZ = CPR == 16 ? 128 : 16;  // of 8 keys further on
   auto k_fragment = [&](int t, int kk) {
     return __builtin_bit_cast(
         bf16x8, *(const __attribute__((address_space(3))) u32x4*)((ka ^ kk * 32) + t * 32 * ROW));
