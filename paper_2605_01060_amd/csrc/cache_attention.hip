@@ -4,8 +4,39 @@
 //   p_k = exp(scale Q[t, h] . K[k, h / G]) over the positions that row t sees,
 //
 // G = heads per key head; a row that sees none gives zeros.  The G query heads
-// that share a key head are rows of one matrix: row r of (sequence, key head)
-// is query r / G, head r % G of the group.
+// that share a key head are rows of one matrix: row r of (sequence, key head) is
+// query r / G, head r % G of the group.
+//
+// A code is decoded to bf16 exactly, two by one instruction that takes the scale's
+// exponent, so what is rounded is what cross attention rounds: the probabilities to
+// bf16 for their product with V, not in their sum.  S^T = K Q^T and O^T += V^T P^T,
+// so that a lane owns a row's maximum, sum and rescaling and the probabilities are
+// the second product's operand where they are.  Three arrangements, by the rows of a
+// (sequence, key head) in the call:
+//
+// Up to 16 or 32 rows (a step, drafts): waves with blocks of 32 keys of their own
+// against all rows in 16x16x32 MFMAs.  A lane loads a quarter of a key, whose codes
+// are the MFMA's operand as they come (the order of the features is one for both
+// operands), so K needs no LDS; V goes through it to be read transposed.  The next
+// block's codes are loaded while one is computed (two ahead changed nothing).  Bound
+// by memory where there is much of it: one query of 32 / 8 heads x 128 over 100,003
+// keys takes 23 us, its keys streamed at 6.4 TB/s once they stream, 48 x about 8,000
+// keys 79 us, 5.5 TB/s.  The VALU is half busy then, a half of it decoding.
+//
+// 64 or 128 rows a tile (prompts, many drafts): four waves decode blocks of 64 keys
+// into LDS together, a block ahead, and take 32x32x16 MFMAs from there; for 64 rows
+// two waves share 32 rows and halve the keys (64 x 16 queries x 3001 keys, 16 / 4 x
+// 128: 97 -> 61 us against waves with keys of their own).  8 x 2048 queries x 8192
+// keys, 16 x 128: 1,040 us, 1,060 TFLOP/s, 16 x 64 613 us, 897 TFLOP/s, 16 x 32 480
+// us; what bounds it is the power limit and the VALU, as in cross attention.  Blocks
+// of 32 keys with three units a CU were 4 to 11 % slower here.
+//
+// Lengths are known on the device alone.  Where a unit (a tile of a sequence and key
+// head) has a long way to go and units are few, all units' blocks of keys are shared
+// out evenly to as many workgroups as the chip holds, each of which finds its share
+// from the lengths (2.3 us); a second kernel joins the parts of a unit that is cut.
+// 4 x about 1500 queries x about 6000 keys, 16 / 4 x 128: 402 us with a unit a
+// workgroup, 246 so.  Otherwise a unit is a workgroup's, longest first.
 #include <float.h>
 #include <math.h>
 
@@ -333,7 +364,8 @@ __device__ __forceinline__ uint32_t v_slot(int key, int chunk) {
 }
 
 // Few rows: RT tiles of 16 against blocks of 32 keys, each wave of four with
-// blocks of its own.
+// blocks of its own.  Maxima and sums are a lane's own over its keys (a quarter of
+// them) and joined at the end; so are the waves.
 template <int DH, int RT>
 __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Unit& u) {
   constexpr int STEPS = DH / 32, FT = DH / 16, CPR = DH / 8, WAVES = 4;
@@ -997,11 +1029,17 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
   const int64_t rows = max_rows * group;
   const int cls = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
   s.tile_rows = 16 << cls;
-  s.block_shift = cls >= 2 ? 6 : 7;  // few rows: 32 keys for each wave
+  s.block_shift = cls >= 2 ? 6 : 7;  // few rows: 32 keys for each of four waves
   s.tiles = (rows + s.tile_rows - 1) / s.tile_rows;
   s.units = n_seqs * n_kv_heads * s.tiles;
   const int64_t workers = (int64_t)n_cus * PLACES[cls][d_head / 64] / 8 * 8;
   const int64_t most = ((max_length - 1) >> s.block_shift) + 1;  // blocks of a unit
+  // Sharing costs 2 us to find the shares and 5 us for the join, or 13 where tiles'
+  // parts are 64 KiB each, a block 1 us (64 keys for a tile, 128 for few rows).  It is
+  // left where units are short or fill the chip twice over.  Measured, a unit a
+  // workgroup / shared, us: 1 x 1000 queries x 1000 keys, 16 / 4 x 128 27 / 56; 200 x 4
+  // x 500, 12 x 64 23 / 45; 8 x 2048 x 8192, 16 x 128 1047 / 1144; 1 x 512 x 30,000,
+  // 16 / 4 x 128 400 / 146; 48 x 1 x about 8000, 32 / 8 x 128 96 / 87.
   s.least_share = cls >= 2 ? 8 : 2;
   s.workers = 0;
   if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) && s.units <= 2 * workers)
