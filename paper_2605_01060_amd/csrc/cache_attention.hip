@@ -197,93 +197,136 @@ __device__ __forceinline__ int last_upto(const int* before, int at) {
   return uniform(n);
 }
 
+// The largest of the workgroup's values, none below 0.
+__device__ __forceinline__ int most_of(int v, int* s_wave) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true));  // as scan64
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true));
+  if ((threadIdx.x & 63) == 63) s_wave[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return uniform(max(max(s_wave[0], s_wave[1]), max(s_wave[2], s_wave[3])));
+}
+
+// The workgroup's number among `active` ones, -1 without one: those of one XCD
+// follow each other, and every XCD has as many.
+__device__ __forceinline__ int worker_of(int active) {
+  const int each = (active + 7) >> 3, mine = (int)blockIdx.x >> 3;
+  const int worker = ((int)blockIdx.x & 7) * each + mine;
+  return mine < each && worker < active ? worker : -1;
+}
+
 // The workgroup's part of all units' blocks of keys.  Workgroups of one XCD have
 // parts next to each other, of a sequence's keys, in the order of sequence, tile,
-// key head.
+// key head; every XCD has as many.
 //
-// Few units are cut into equal parts each, as many as keep them to the share of a
-// worker, so that no worker has two (16 sequences, 5 queries, 3001 keys, 16 / 4 x
-// 128: a unit's start and end take 5 us, a block 1.6).  Of more units each worker
-// has an equal share, which starts and ends anywhere.  The parts of a unit that is
-// cut are joined afterwards; who has the last one knows where they started.
-template <class Body>
-__device__ __forceinline__ void shared_units(const CacheAttention& a, Body body) {
-  __shared__ int s_before[256], s_wave[3][4];  // what lies before a thread's (sequence, tile) pairs
+// Few units are cut into equal parts, the most that the workers suffice for, so that
+// no worker has two: a unit's start and end take 5 us.  Of more units each worker has
+// an equal share, which starts and ends anywhere, or, where they are no more than the
+// workers and the longest is within what a cut would save (`fit`), a whole unit.  The
+// parts of a unit that is cut are joined afterwards; who has the last one knows where
+// they started.  Measured, us, a unit a workgroup / equal shares / equal parts:
+//   16 x 5 queries x about 3001 keys, 16 / 4 x 128    40 / 24 / 20
+//   64 x 5 x about 3001, 16 / 4 x 128                 42 / 40 / 44
+//   48 x 1 x about 8000, 32 / 8 x 128                 112 / 87 / 100
+//   64 x 4 x 4000, 32 / 8 x 128                       53 / 70 / 58 (uncut, of which 3
+//                                                     find the shares, 3 the join)
+template <class Fit, class Body>
+__device__ __forceinline__ void shared_units(const CacheAttention& a, Fit fit, Body body) {
+  __shared__ int s_before[256], s_wave[5][4];  // what lies before a thread's (sequence, tile) pairs
   __shared__ Sequence s_first[256];            // its first sequence
-  const int worker = (int)(blockIdx.x % 8) * (a.workers / 8) + (int)(blockIdx.x / 8);
   const int pairs = a.c.n_seqs * a.tiles, per = (pairs + 255) >> 8, heads = a.c.n_kv_heads;
-  int mine = 0;
+  int mine = 0, most = 0, some = 0;  // blocks, the most of a pair, pairs with any
   for (int i = 0; i < per; ++i) {
     const int pair = (int)threadIdx.x * per + i;
     if (pair >= pairs) break;
     const int seq = over(pair, a.by_tiles);
     const Sequence s = sequence_of(a, seq);
     if (i == 0) s_first[threadIdx.x] = s;
-    mine += blocks_of(a, s, pair - seq * a.tiles) * heads;
+    const int n = blocks_of(a, s, pair - seq * a.tiles);
+    mine += n;
+    most = max(most, n);
+    some += n > 0;
   }
-  const int2 blocks = sums_before(mine, s_wave[0]);
-  const int total = blocks.y;
-  if (a.units <= a.workers / 4) {  // (a pair a thread then)
+  // Units are cut into parts of at most `cut` blocks, of which a worker has `take`.
+  int2 parts = sums_before(mine * heads, s_wave[0]);
+  const int total = parts.y;
+  int cut = 1, take = max(over(total + a.workers - 1, a.by_workers), a.least_share);
+  if (a.units <= a.workers / 4 && per == 1) {
     // The least share, if its parts are no more than the workers, else one that is
     // sure to be.
-    const int n_mine = over(mine, a.by_heads);
-    int share = max(over(total + a.workers - 1, a.by_workers), a.least_share);
-    int2 parts = sums_before((n_mine + share - 1) / share * heads, s_wave[1]);
+    cut = take;
+    take = 1;
+    parts = sums_before((mine + cut - 1) / cut * heads, s_wave[1]);
     if (parts.y > a.workers) {
-      share = max((total + a.workers - a.units - 1) / (a.workers - a.units), a.least_share);
-      parts = sums_before((n_mine + share - 1) / share * heads, s_wave[2]);
+      cut = max((total + a.workers - a.units - 1) / (a.workers - a.units), a.least_share);
+      parts = sums_before((mine + cut - 1) / cut * heads, s_wave[2]);
     }
-    s_before[threadIdx.x] = parts.x;
-    __syncthreads();
-    if (worker >= parts.y) return;
-    const int pair = last_upto(s_before, worker);
-    const Sequence s = uniform(s_first[pair]);
-    const int seq = over(pair, a.by_tiles), tile = pair - seq * a.tiles;
-    const int n = blocks_of(a, s, tile), cuts = (n + share - 1) / share, size = (n + cuts - 1) / cuts;
-    const int past = worker - uniform(s_before[pair]), kvh = past / cuts, part = past - kvh * cuts;
-    Unit u = unit_of(a, s, seq, kvh, tile);
-    u.whole = cuts == 1;
-    u.k0 = part * size << a.block_shift;
-    u.k1 = min((part + 1) * size << a.block_shift, u.limit);
-    u.slot = 2 * worker + (part == 0);
-    if (part == cuts - 1 && threadIdx.x == 0)
-      a.joins[pair * heads + kvh] = make_int2(u.whole ? -1 : worker - part, worker);
-    body(u);
-    return;
+  } else if (a.units <= a.workers && fit(take, most_of(most, s_wave[3]))) {
+    cut = INT32_MAX >> 1;
+    take = 1;
+    parts = sums_before(some * heads, s_wave[4]);
   }
-  s_before[threadIdx.x] = blocks.x;
+  s_before[threadIdx.x] = parts.x;
   __syncthreads();
-  const int share = max(over(total + a.workers - 1, a.by_workers), a.least_share);
-  int at = worker * share;
-  const int end = min(at + share, total);
-  if (at >= end) return;
+  const int worker = worker_of((parts.y + take - 1) / take);
+  if (worker < 0) return;
+  int at = worker * take;
+  const int end = min(at + take, parts.y);
   const int thread = last_upto(s_before, at);
   int start = uniform(s_before[thread]);
   Sequence s = uniform(s_first[thread]);
-  for (int pair = thread * per, of = -1; at < end; ++pair) {
-    const int seq = over(pair, a.by_tiles), tile = pair - seq * a.tiles;
-    if (of >= 0 && of != seq) s = uniform(sequence_of(a, seq));
-    of = seq;
-    const int n = blocks_of(a, s, tile);
-    if (at >= start + n * heads) {
-      start += n * heads;
-      continue;
+  // (A part of one unit has code of its own: what is in a loop over units is
+  // scheduled for fewer registers, 3 to 7 % slower.)
+  int pair = thread * per, seq = over(pair, a.by_tiles), tile = pair - seq * a.tiles;
+  int n = 0, cuts = 0;
+  while (true) {
+    n = blocks_of(a, s, tile);
+    cuts = (n + cut - 1) / cut;
+    if (at < start + cuts * heads) break;
+    start += cuts * heads;
+    if (++tile == a.tiles) {
+      tile = 0;
+      s = uniform(sequence_of(a, ++seq));
     }
-    const int past = (at - start) / n;
-    start += past * n;
-    for (int kvh = past; kvh < heads && at < end; ++kvh, start += n) {
-      Unit u = unit_of(a, s, seq, kvh, tile);
-      const int from = at - start, to = min(n, end - start);
-      u.whole = from == 0 && to == n;
-      u.k0 = from << a.block_shift;
-      u.k1 = min(to << a.block_shift, u.limit);
-      u.slot = 2 * worker + (from == 0);
-      body(u);
-      if (to == n && threadIdx.x == 0)
-        a.joins[pair * heads + kvh] = make_int2(u.whole ? -1 : start / share, worker);
-      at = start + to;
-      if (at < end) __syncthreads();  // LDS is read out
-    }
+    ++pair;
+  }
+  int kvh = (at - start) / cuts;
+  start += kvh * cuts;
+  auto part_of = [&](int from, int to) {
+    const int size = (n + cuts - 1) / cuts;
+    Unit u = unit_of(a, s, seq, kvh, tile);
+    u.whole = from == 0 && to == cuts;
+    u.k0 = from * size << a.block_shift;
+    u.k1 = min(to * size << a.block_shift, u.limit);
+    u.slot = 2 * worker + (from == 0);
+    if (to == cuts && threadIdx.x == 0)
+      a.joins[pair * heads + kvh] = make_int2(u.whole ? -1 : start / take, worker);
+    return u;
+  };
+  if (take == 1) {
+    body(part_of(at - start, at - start + 1));
+    return;
+  }
+  while (true) {
+    const int to = min(cuts, end - start);
+    body(part_of(at - start, to));
+    at = start + to;
+    if (at >= end) return;
+    __syncthreads();  // LDS is read out
+    start += cuts;
+    if (++kvh < heads) continue;
+    kvh = 0;
+    do {
+      ++pair;
+      if (++tile == a.tiles) {
+        tile = 0;
+        s = uniform(sequence_of(a, ++seq));
+      }
+      n = cuts = blocks_of(a, s, tile);
+    } while (n == 0);
   }
 }
 
@@ -698,6 +741,11 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
           s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(t, kk), qf[kk], s[t], 0, 0, 0);
       __builtin_amdgcn_s_setprio(0);
       next_block();
+      // V^T of 16 keys is asked for ahead of the exponentials of the 16 before.
+      bf16x8 vf[2][DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) vf[0][dt] = v_fragment(0, dt);
+      __builtin_amdgcn_sched_barrier(0);
       if (key0 + 32 * T > least) {
         asm volatile("");  // a branch around the comparisons, not a selection by both
         const int seen = limit - key0 - 4 * half;
@@ -738,9 +786,14 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
           l_run += p;
           pb[r] = (__bf16)p;
         }
+        if (c + 1 < 2 * T) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) vf[c + 1 & 1][dt] = v_fragment(c + 1, dt);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(c, dt), pb, o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c & 1][dt], pb, o[dt], 0, 0, 0);
       }
     } else {
       next_block();
@@ -825,7 +878,10 @@ template <int DH, int RT, bool SHARED>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(PLACES[RT / 2][DH / 64]))) void few_rows_kernel(CacheAttention a) {
   auto body = [&](const Unit& u) { few_rows_unit<DH, RT>(a, u); };
-  if constexpr (SHARED) shared_units(a, body);
+  // Half of the places of 16 rows stream as much as the memory gives; a join takes as
+  // long as six blocks.
+  auto fit = [](int share, int most) { return most <= share * (RT == 1 ? 2 : 1) + 6; };
+  if constexpr (SHARED) shared_units(a, fit, body);
   else one_unit(a, body);
 }
 
@@ -833,7 +889,8 @@ template <int DH, int GROUPS, bool SHARED>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(SHARED ? PLACES[GROUPS / 2 + 1][DH / 64] : 2))) void tile_kernel(CacheAttention a) {
   auto body = [&](const Unit& u) { tile_unit<DH, GROUPS>(a, u); };
-  if constexpr (SHARED) shared_units(a, body);
+  auto fit = [](int, int) { return false; };  // (equal shares are as fast with even lengths)
+  if constexpr (SHARED) shared_units(a, fit, body);
   else one_unit(a, body);
 }
 
@@ -1042,7 +1099,8 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
   // 16 / 4 x 128 400 / 146; 48 x 1 x about 8000, 32 / 8 x 128 96 / 87.
   s.least_share = cls >= 2 ? 8 : 2;
   s.workers = 0;
-  if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) && s.units <= 2 * workers)
+  if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) &&
+      s.units <= (cls >= 2 ? 2 : 1) * workers)
     s.workers = workers;
   return s;
 }

@@ -379,7 +379,7 @@ def test_attention_over_long_sequences(lengths, rows, page, heads, hk, dh, causa
 # sequences without rows or keys.
 BATCHES = [(60, 1, 3000, 64, 32, 8, 128), (300, 1, 2500, 32, 4, 1, 64), (700, 2, 1400, 16, 2, 1, 32),
            (40, 7, 2200, 64, 12, 4, 128), (90, 9, 1500, 32, 6, 2, 64), (7, 350, 3000, 64, 8, 4, 128),
-           (30, 12, 2600, 64, 16, 4, 64), (500, 1, 1300, 128, 8, 8, 32), (6, 260, 2500, 16, 9, 9, 32)]
+           (30, 12, 2600, 64, 16, 4, 64), (400, 1, 2100, 32, 2, 1, 32), (200, 4, 1800, 64, 4, 2, 128), (500, 1, 1300, 128, 8, 8, 32), (6, 260, 2500, 16, 9, 9, 32)]
 
 
 @pytest.mark.parametrize("seqs,rows,length,page,heads,hk,dh", BATCHES)
