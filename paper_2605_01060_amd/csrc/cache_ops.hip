@@ -127,7 +127,7 @@ surge_status attention_shape(const surge_kv_cache* c, int64_t max_rows, int32_t 
 surge_status check_heads(const surge_kv_cache* c, int64_t max_rows, int32_t n_heads) {
   if (n_heads < 1 || n_heads > kMaxHeads || n_heads % c->n_kv_heads)
     return fail(SURGE_ERR_INVALID_ARGUMENT, "n_heads=%d, n_kv_heads=%d", n_heads, c->n_kv_heads);
-  if (max_rows < 0 || max_rows * n_heads > kMostLength)
+  if (max_rows < 0 || max_rows > kMostLength / n_heads)
     return fail(SURGE_ERR_INVALID_ARGUMENT, "max_rows=%lld", (long long)max_rows);
   return SURGE_OK;
 }

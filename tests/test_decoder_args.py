@@ -126,3 +126,11 @@ def test_no_rows_or_sequences_is_a_call_that_does_nothing():
     S.surge_op_verify_drafts(**{**VERIFY, "n_seqs": 0})
     assert S.surge_cache_attention_workspace(cache(n_seqs=0), 4, 4) == 0
     assert S.surge_cache_attention_workspace(cache(), 0, 4) == 0
+
+
+@pytest.mark.parametrize("max_rows", [1 << 62, (1 << 62) + 1, (1 << 63) - 1, 1 << 54, (1 << 28) + 1])
+def test_refused_max_rows_whose_product_with_the_heads_wraps(max_rows):
+    """2^62 rows of 4 heads are 2^64, 0 in 64 bits."""
+    refused(S.surge_op_cache_attention, ATTEND, cache=cache(), max_rows=max_rows)
+    with pytest.raises(S.SurgeError):
+        S.surge_cache_attention_workspace(cache(), max_rows, 4)
