@@ -284,8 +284,8 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
  * The rows of a call are packed as the texts of a SuperBatch: sequence i has
  * rows d_cu[i] .. d_cu[i+1]-1 (device int32 [n_seqs+1], never decreasing, from
  * 0) of n_rows in all, or n_rows / n_seqs each where d_cu is NULL.  They are its
- * last positions: of n rows, row r is position length - n + r.  Rows of the
- * matrices behind the last sequence are neither read nor written.
+ * last positions: of n rows, row r is position length - n + r.  What stands in
+ * the matrices' rows behind the last sequence does not matter, and stays.
  *
  * d_pages 16-byte aligned; n_pages below 2^31; n_kv_heads at most 1024; n_seqs
  * at most 2^20; ld_table at least max_length / page_tokens, rounded up;
@@ -310,9 +310,10 @@ surge_status surge_cache_page_bytes(int32_t page_tokens, int32_t n_kv_heads, int
  * of one projection's output, say) quantized and written to their positions.  Of
  * 32 features with a = max(max |x|, 2^-100) the scale s is the least power of two
  * with a <= 7 s, at most 2^125, and a code stands for the number nearest to x / s
- * (ties to the even code, beyond 6 is 6): off by s at most, below 4 s by s / 2, below 2 s
- * by s / 4.  32 features with an infinity or a NaN are marked as NaN.  Rows of negative
- * positions (more rows than the sequence is long) are not written.
+ * (ties to the even code, beyond 6 is 6): off by s at most (magnitudes beyond 7 2^125 by
+ * 2 s), below 4 s by s / 2, below 2 s by s / 4.  32 features with an infinity or a NaN are
+ * marked as NaN.  Rows of negative positions (more rows than the sequence is long) are
+ * not written.
  */
 surge_status surge_op_cache_write(const surge_kv_cache* cache, int64_t n_rows, const int32_t* d_cu,
                                   const uint16_t* d_k, int64_t ld_k, const uint16_t* d_v, int64_t ld_v,
@@ -363,9 +364,9 @@ surge_status surge_op_cache_attention(const surge_kv_cache* cache, int64_t n_row
  * ones one more token is drawn, the least v with sum_{w <= v} r(w) > u_last
  * sum_w r(w), where r is max(p_a - q_a, 0) of the first rejected draft a, or p_n
  * after n accepted ones.  Without d_q drafts are certain: q_j is 1 at x_j.  Where
- * nothing of r is above 0, r is p_a.  Comparisons and sums are in 64 bits; a
- * probability that is not above 0 (NaN too) counts as 0, and a row whose sum is
- * infinite or 0 gives token -1.
+ * nothing of r is above 0, r is p_a.  Comparisons and sums are in 64 bits.  A draft
+ * with a NaN in its comparison is not accepted, an r(w) that is not above 0 (NaN
+ * too) counts as 0, and a row whose sum is infinite or 0 gives token -1.
  * d_p, d_q fp32 rows of vocab (at most 2^22) probabilities, ld_p and ld_q apart;
  * d_u fp32 [n_seqs, max_drafts + 1], u_j at j, u_last in the last column.
  * Outputs: d_tokens int32 [n_seqs, max_drafts + 1], the accepted drafts, the drawn

@@ -714,6 +714,114 @@ def test_verify_takes_the_token_on_either_side_of_a_border():
 
 
 # ---------------------------------------------------------------------------
+# Far ends of what may be asked for
+# ---------------------------------------------------------------------------
+
+def test_rows_whose_offsets_pass_32_bits():
+    """Five column ranges of one matrix of the widest rows: written, read, attended."""
+    torch = torch_cuda()
+    n, ld, w = 1100, 1 << 22, 128
+    big = torch.empty(n * ld, dtype=torch.bfloat16, device="cuda").view(n, ld)
+    k, v, q, out, back = (big[:, i * 256:i * 256 + w] for i in range(5))
+    g = gen(1)
+    for x in (k, v, q):
+        x.copy_(randn(g, n, w).bfloat16())
+    c = Cache([1200, 30], 32, 2, 64, 3, fill=0)
+    rows, cu = [1080, 20], dev([0, 1080, 1100])
+    c.fill(5)
+    seq, pos = places(c.lengths_np, rows)
+    S.surge_op_cache_write(c.desc, n, cu, k, ld, v, ld)
+    S.surge_op_cache_read(c.desc, n, cu, out, ld, back, ld)
+    assert torch.equal(out.double(), values(*quantized(k)))
+    assert torch.equal(back.double(), values(*quantized(v)))
+    for i, (first, size) in enumerate(((0, 1080), (1080, 20))):
+        for t, x in enumerate((k, v)):
+            c.held[i][t][-size:] = values(*quantized(x[first:first + size])).view(size, 2, 64)
+    for wide in (rows, [1, 20]):
+        m = sum(wide)
+        at = big[n - m:]
+        q, out = at[:, 512:512 + w], at[:, 768:768 + w]
+        attend(c, q, wide, 2, True, out)
+        within(out, *reference(c, q.contiguous(), wide, 2, True))
+
+
+def test_verify_rows_whose_offsets_pass_32_bits():
+    torch = torch_cuda()
+    n, k, ld = 2, 1, 1 << 30
+    for vocab in (100, 40_000):  # one launch and two
+        p, q, drafts, u = draft_inputs(n, k, vocab, vocab)
+        far = torch.empty(((k + 1) * n - 1) * ld + vocab, device="cuda")
+        far_p = far.as_strided((n, k + 1, vocab), ((k + 1) * ld, ld, 1))
+        far_p.copy_(p)
+        far_q = far.as_strided((n, k, vocab), (k * ld, ld, 1), 1 << 29)
+        far_q.copy_(q)
+        for probs in (far_q, None):
+            for u0 in (0.0, 1.0):  # accepted, rejected
+                u[:, 0] = u0
+                want = verified(p, None if probs is None else q, drafts, [k] * n, u)
+                tokens = torch.empty(n, k + 1, dtype=torch.int32, device="cuda")
+                accepted = torch.empty(n, dtype=torch.int32, device="cuda")
+                ws = torch.empty(max(16, S.surge_verify_workspace(n, vocab)), dtype=torch.uint8, device="cuda")
+                S.surge_op_verify_drafts(n, k, vocab, None, drafts, far_p, ld, probs, ld, u, ws, tokens, accepted)
+                assert np.array_equal(tokens.cpu().numpy(), want[0])
+                assert np.array_equal(accepted.cpu().numpy(), want[1])
+
+
+def test_attention_of_a_hundred_thousand_sequences():
+    """Of length 0, zeros, or 1: the value itself, whatever the score."""
+    torch = torch_cuda()
+    n, hk, dh = 100_003, 2, 32
+    lengths = np.random.default_rng(1).integers(0, 2, n)
+    c = Cache(lengths, 16, hk, dh, 1)
+    g = gen(1)
+    k, v, q = (randn(g, n, w).bfloat16() for w in (hk * dh, hk * dh, 2 * hk * dh))
+    S.surge_op_cache_write(c.desc, n, None, k, hk * dh, v, hk * dh)
+    out = torch.empty_like(q)
+    attend(c, q, [1] * n, 2 * hk, True, out)
+    held = values(*quantized(v)) * torch.from_numpy(lengths).cuda()[:, None]
+    assert torch.equal(out.double().view(n, hk, 2, dh), held.view(n, hk, 1, dh).expand(n, hk, 2, dh))
+
+
+@pytest.mark.parametrize("rows", [[2, 3], [60, 70]])
+def test_attention_with_pages_shared_by_sequences(rows):
+    """Two sequences that begin alike, with the same pages."""
+    c = Cache([700, 900], 64, 2, 64, 1)
+    c.table_np[1, :9] = c.table_np[0, :9]
+    c.table.copy_(dev(c.table_np))
+    c.fill(3)
+    for w in range(2):
+        c.held[0][w][:9 * 64] = c.held[1][w][:9 * 64]  # written last
+    check(c, rows, 8, True, 4)
+
+
+@pytest.mark.parametrize("rows", [[1, 1, 2], [40, 40, 40], [100, 3, 100]])
+def test_attention_of_lengths_out_of_range(rows):
+    """Below 0 is 0, beyond max_length is max_length."""
+    torch = torch_cuda()
+    c = Cache([0, 5000, 100], 16, 2, 64, 1).fill(2)
+    c.lengths.copy_(dev([-5, (1 << 31) - 1, 100]))
+    check(c, rows, 2, True, 4)
+    check(c, rows, 2, False, 4)
+
+
+def test_attention_over_caches_of_no_length():
+    """max_length 0: a table without entries, every row zeros."""
+    torch = torch_cuda()
+    pages = torch.zeros(1, S.surge_cache_page_bytes(16, 2, 64), dtype=torch.uint8, device="cuda")
+    c = S.KVCache(pages, 1, 16, 2, 64, dev([0]), 0, 3, dev([0, 7, -1]), 0)
+    for rows in (1, 200):
+        assert S.surge_cache_attention_workspace(c, rows, 4) == 0
+        q = randn(gen(1), 3 * rows, 256).bfloat16()
+        out = torch.full_like(q, 7.0)
+        S.surge_op_cache_attention(c, 3 * rows, None, rows, 4, True, 0.125, q, 256, None, out, 256)
+        assert (out == 0).all()
+        S.surge_op_cache_write(c, 3 * rows, None, q, 256, q[:, 128:], 256)
+        back = torch.full_like(q, 7.0)
+        S.surge_op_cache_read(c, 3 * rows, None, back, 256, back[:, 128:], 256)
+        assert (back == 0).all() and (pages == 0).all()
+
+
+# ---------------------------------------------------------------------------
 # The operators together: a step of a decoder
 # ---------------------------------------------------------------------------
 
