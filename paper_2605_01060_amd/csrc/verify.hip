@@ -138,12 +138,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const float* row, i
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(row), 0, row ? vocab * 4 : 0, 0x00027000);
 }
 
-__device__ __forceinline__ Row row_of(const VerifyDrafts& a, int64_t seq, int n, int acc) {
+__device__ __forceinline__ Row row_of(const VerifyDrafts& a, int64_t seq, int acc, bool rejected) {
   Row r;
-  r.has_q = acc < n && a.q;
+  r.has_q = rejected && a.q;
   r.p = row_buffer(a.p + (seq * (a.max_drafts + 1) + acc) * a.ld_p, a.vocab);
   r.q = row_buffer(r.has_q ? a.q + (seq * a.max_drafts + acc) * a.ld_q : nullptr, a.vocab);
-  r.without = acc < n && !a.q ? a.drafts[seq * a.max_drafts + acc] : -1;
+  r.without = rejected && !a.q ? a.drafts[seq * a.max_drafts + acc] : -1;
   return r;
 }
 
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(64 * WAVES) void verify_kernel(VerifyDrafts a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, v = (int)threadIdx.x * 4;
   int n;
   const int acc = accepted_drafts(a, seq, &n);
-  Row r = row_of(a, seq, n, acc);
+  Row r = row_of(a, seq, acc, acc < n);
   Tokens<N> t;
   t.load(r, v);
   double of_tile, upto, total;
@@ -284,15 +284,17 @@ __global__ __launch_bounds__(64 * WAVES) void verify_kernel(VerifyDrafts a) {
   choose_token(a, seq, acc, w, v + tile * TILE, before, target);
 }
 
-// The tiles' sums of the row that decides, a workgroup for each TILES of them.
-__global__ __launch_bounds__(64 * WAVES) void verify_sum_kernel(VerifyDrafts a, int groups, int tiles) {
+// The tiles' sums of the row that decides, a workgroup for each TILES of them, and
+// 2 accepted drafts + (one is rejected) of a sequence.
+__global__ __launch_bounds__(64 * WAVES) void verify_sum_kernel(VerifyDrafts a, int groups, int tiles, int* taken) {
   __shared__ double shared[WAVES][TILES];
   const int64_t seq = blockIdx.x / (unsigned)groups;
   const int first = (int)(blockIdx.x % (unsigned)groups) * TILES;
   const int v = first * TILE + (int)threadIdx.x * 4;
   int n;
   const int acc = accepted_drafts(a, seq, &n);
-  const Row r = row_of(a, seq, n, acc);
+  const Row r = row_of(a, seq, acc, acc < n);
+  if (first == 0 && threadIdx.x == 0) taken[seq] = 2 * acc + (acc < n);
   Tokens<TILES> t;
   t.load(r, v);
   double s[TILES];
@@ -308,16 +310,15 @@ __global__ __launch_bounds__(64 * WAVES) void verify_sum_kernel(VerifyDrafts a, 
   }
 }
 
-__global__ __launch_bounds__(64 * WAVES) void verify_choose_kernel(VerifyDrafts a, int tiles) {
+__global__ __launch_bounds__(64 * WAVES) void verify_choose_kernel(VerifyDrafts a, int tiles, const int* taken) {
   __shared__ double shared[WAVES][1];
   const int64_t seq = blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   double* const sums = a.sums + seq * tiles;
+  const int mark = taken[seq], acc = mark >> 1;
+  Row r = row_of(a, seq, acc, mark & 1);
   double total = 0.0;
   for (int i = 0; i < tiles; i += 64) total += lane_of(scan64(i + lane < tiles ? sums[i + lane] : 0.0), 63);
-  int n;
-  const int acc = accepted_drafts(a, seq, &n);
-  Row r = row_of(a, seq, n, acc);
   Tokens<1> t;
   if (!(total > 0.0) && (r.has_q || r.without >= 0)) {
     // Nothing left over by q: the target's own probabilities.
@@ -370,7 +371,7 @@ int tiles_of(int vocab) { return (vocab + TILE - 1) / TILE; }
 
 int64_t verify_workspace(int64_t n_seqs, int vocab) {
   const int tiles = tiles_of(vocab);
-  return tiles > TILES ? n_seqs * tiles * (int64_t)sizeof(double) : 0;
+  return tiles > TILES ? n_seqs * (tiles * (int64_t)sizeof(double) + (int64_t)sizeof(int)) : 0;
 }
 
 hipError_t launch_verify_drafts(int64_t n_seqs, const VerifyDrafts& a, hipStream_t stream) {
@@ -382,8 +383,9 @@ hipError_t launch_verify_drafts(int64_t n_seqs, const VerifyDrafts& a, hipStream
     hipLaunchKernelGGL(verify_kernel<TILES>, seqs, block, 0, stream, a);
   } else {
     const int groups = (tiles + TILES - 1) / TILES;
-    hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)(n_seqs * groups)), block, 0, stream, a, groups, tiles);
-    hipLaunchKernelGGL(verify_choose_kernel, seqs, block, 0, stream, a, tiles);
+    int* const taken = reinterpret_cast<int*>(a.sums + n_seqs * tiles);
+    hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)(n_seqs * groups)), block, 0, stream, a, groups, tiles, taken);
+    hipLaunchKernelGGL(verify_choose_kernel, seqs, block, 0, stream, a, tiles, taken);
   }
   return hipGetLastError();
 }
