@@ -19,15 +19,15 @@
 // are the MFMA's operand as they come (the order of the features is one for both
 // operands), so K needs no LDS; V goes through it to be read transposed.  The next
 // block's codes are loaded while one is computed (two ahead changed nothing).  Bound
-// by memory where there is much of it: one query of 32 / 8 heads x 128 over 100,003
-// keys takes 23 us, its keys streamed at 6.4 TB/s once they stream, 48 x about 8,000
-// keys 79 us, 5.5 TB/s.  The VALU is half busy then, a half of it decoding.
+// by memory where there is much of it: one query of 32 / 8 heads x 128 over 48 x about
+// 8,000 keys takes 82 us, 5.3 TB/s, over 100,003 keys 25 us, of which the first 4 find
+// the share and the first codes.  The VALU is half busy then, a half of it decoding.
 //
 // 64 or 128 rows a tile (prompts, many drafts): four waves decode blocks of 64 keys
 // into LDS together, a block ahead, and take 32x32x16 MFMAs from there; for 64 rows
 // two waves share 32 rows and halve the keys (64 x 16 queries x 3001 keys, 16 / 4 x
 // 128: 97 -> 61 us against waves with keys of their own).  8 x 2048 queries x 8192
-// keys, 16 x 128: 1,040 us, 1,060 TFLOP/s, 16 x 64 613 us, 897 TFLOP/s, 16 x 32 480
+// keys, 16 x 128: 1,044 us, 1,053 TFLOP/s, 16 x 64 607 us, 905 TFLOP/s, 16 x 32 471
 // us; what bounds it is the power limit and the VALU, as in cross attention.  Blocks
 // of 32 keys with three units a CU were 4 to 11 % slower here.
 //
@@ -36,7 +36,7 @@
 // out evenly to as many workgroups as the chip holds, each of which finds its share
 // from the lengths (2.3 us); a second kernel joins the parts of a unit that is cut.
 // 4 x about 1500 queries x about 6000 keys, 16 / 4 x 128: 402 us with a unit a
-// workgroup, 246 so.  Otherwise a unit is a workgroup's, longest first.
+// workgroup, 247 so.  Otherwise a unit is a workgroup's, longest first.
 #include <float.h>
 #include <math.h>
 

@@ -3,13 +3,20 @@
 // Every 32 values of a row have a scale s = 2^e, the least with a <= 7 s for
 // a = max(max |x|, 2^-100) (at most 2^125), and the 4-bit float nearest to x / s
 // each (+-0, 0.5, 1, 1.5, 2, 3, 4, 6; ties to the even code; what rounds beyond 6
-// is 6, off by s at most like the values between 4 and 6).  With a scale of a
+// is 6, off by s at most like the values between 4 and 6, but for magnitudes beyond
+// 7 2^125, the largest scale's, off by 2 s).  With a scale of a
 // power of two both steps are exact but for that one rounding, and a code times
 // its scale is a bf16: reading back rounds nothing.
 //
 // A wave takes 16 rows of one key head: 8 features a lane, so that it reads 16
-// bytes a lane, 64 to 256 of a row together, and writes the codes of
-// neighbouring tokens, which lie behind each other in a page, together too.
+// bytes a lane, 128 or 256 of a row together, and writes the codes of
+// neighbouring tokens, which lie behind each other in a page, together too.  Bound
+// by memory, or in small calls by a chain of three loads (offsets, length, table):
+// 100,003 rows x 8 x 128 are written in 77 us, 6.7 TB/s, most of it read, and read
+// back in 103, 5.0 TB/s, most of it written; a copy moves 4.95.  64 rows take 4.7 us.
+// Rows are loaded and stored past the caches (nontemporal), places found once for
+// four heads and neighbouring rows kept on one XCD: 192,000 rows x 12 x 64, written
+// and read, 383 us without them, 256 with.
 #include "cache_device.h"
 
 namespace surge {

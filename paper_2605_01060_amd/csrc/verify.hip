@@ -14,7 +14,10 @@
 //
 // A small call is a chain of latencies: the drafts, their probabilities, the row,
 // then sums and scans.  Those are lane exchanges in registers and two barriers,
-// each wave finding the tile and the wave that the sum passes in for itself.
+// each wave finding the tile and the wave that the sum passes in for itself (through
+// LDS 15.7 us a call, so 7.5, most of it the caller's).  256 x 6 drafts of 100,003
+// tokens take 43 us, 37 of them the sums, 5.5 TB/s; with a workgroup a sequence, row
+// by row, 133.
 #include "cache_device.h"
 
 namespace surge {
