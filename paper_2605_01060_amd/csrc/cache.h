@@ -55,6 +55,7 @@ struct CacheAttention {
   float scale_log2;   // scale * log2(e)
   // Of cache_attention_shape.
   int tile_rows, block_shift, tiles, units, workers, least_share;
+  bool wave_units;
   Divisor by_group, by_tiles, by_heads, by_units, by_workers;  // by_units: by n_seqs * n_kv_heads
   // Workspace, where there are workers: of the two slots that each has for the
   // parts of its first and last unit, the rows' maxima (in log2 units) and sums,
@@ -70,6 +71,7 @@ struct CacheAttention {
 // each, or where that is 0 a unit is a workgroup's.
 struct CacheShape {
   int tile_rows, block_shift, least_share;
+  bool wave_units;  // a unit is a wave's
   int64_t tiles, units, workers;
   int64_t slot_rows() const { return 2 * workers * tile_rows; }
   int64_t workspace_bytes(int d_head) const {

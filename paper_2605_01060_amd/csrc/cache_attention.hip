@@ -36,7 +36,8 @@
 // out evenly to as many workgroups as the chip holds, each of which finds its share
 // from the lengths (2.3 us); a second kernel joins the parts of a unit that is cut.
 // 4 x about 1500 queries x about 6000 keys, 16 / 4 x 128: 402 us with a unit a
-// workgroup, 247 so.  Otherwise a unit is a workgroup's, longest first.
+// workgroup, 247 so.  Otherwise a unit is a workgroup's, or a wave's,
+// longest first.
 #include <float.h>
 #include <math.h>
 
@@ -47,7 +48,8 @@
 namespace surge {
 namespace {
 
-// Workgroups of a kernel on a CU, by its class (few rows: 16, 32; tiles of 64, 128) and d_head, that registers and LDS allow.
+// Workgroups of a kernel on a CU, by its class (few rows: 16, 32; tiles of 64, 128) and
+// d_head, that registers and LDS allow.
 constexpr int PLACES[4][3] = {{7, 4, 3}, {5, 3, 2}, {5, 4, 2}, {4, 3, 2}};
 
 // The 16 bytes of codes (d_head 128; 8 or 4 for smaller heads) of a quarter of
@@ -164,10 +166,10 @@ __device__ __forceinline__ int scan64(int v) {
   return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);
 }
 
-// A unit a workgroup, the last tiles first, whose rows see the most keys.
+// A unit a workgroup (or wave), the last tiles first, whose rows see the most keys.
 template <class Body>
-__device__ __forceinline__ void one_unit(const CacheAttention& a, Body body) {
-  const int index = blockIdx.x, of_tile = over(index, a.by_units);
+__device__ __forceinline__ void one_unit(const CacheAttention& a, int index, Body body) {
+  const int of_tile = over(index, a.by_units);
   const int rest = index - of_tile * (a.c.n_seqs * a.c.n_kv_heads), tile = a.tiles - 1 - of_tile;
   const int seq = over(rest, a.by_heads);
   const Sequence s = uniform(sequence_of(a, seq));
@@ -406,18 +408,17 @@ __device__ __forceinline__ uint32_t v_slot(int key, int chunk) {
   return key * 4 + (chunk ^ (key >> 1 & 3));
 }
 
-// Few rows: RT tiles of 16 against blocks of 32 keys, each wave of four with
-// blocks of its own.  Maxima and sums are a lane's own over its keys (a quarter of
-// them) and joined at the end; so are the waves.
-template <int DH, int RT>
+// Few rows: RT tiles of 16 against blocks of 32 keys, each of a unit's WAVES waves (4,
+// or 1: the workgroup has four units) with blocks of its own.  Maxima and sums are a
+// lane's own over its keys (a quarter of them) and joined at the end; so are the waves.
+template <int DH, int RT, int WAVES>
 __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Unit& u) {
-  constexpr int STEPS = DH / 32, FT = DH / 16, CPR = DH / 8, WAVES = 4;
+  constexpr int STEPS = DH / 32, FT = DH / 16, CPR = DH / 8;
   constexpr int STRIDE = DH + 4;  // floats of a staged output row
-  constexpr int LDS_WAVE = (32 * DH * 2 > 16 * STRIDE * 4 ? 32 * DH * 2 : 16 * STRIDE * 4);
-  __shared__ __attribute__((aligned(256))) uint8_t lds[RT * WAVES * LDS_WAVE];
-  __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
+  constexpr int LDS_WAVE = (WAVES == 1 || 32 * DH * 2 > 16 * STRIDE * 4 ? 32 * DH * 2 : 16 * STRIDE * 4);
+  __shared__ __attribute__((aligned(256))) uint8_t lds[(WAVES == 1 ? 1 : RT) * 4 * LDS_WAVE];
   const int lane = own_lane(), col = lane & 15, quarter = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = WAVES == 1 ? 0 : own;
   const int G = a.group;
 
   // Every key waits for the table: it is asked for first.
@@ -449,7 +450,7 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
   }
 
   const int64_t head_at = u.kvh * PageLayout<DH>::head_bytes(a.c.page_shift);
-  u32x4* const sv = reinterpret_cast<u32x4*>(lds + wave * LDS_WAVE);
+  u32x4* const sv = reinterpret_cast<u32x4*>(lds + own * LDS_WAVE);
   int entry = 0;
   Block<DH> next;
   if (block < end) load_block<DH>(a, head_at, pages, 0, block * 32, lane, &next);
@@ -544,8 +545,28 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
         o[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[f], pb[rt], o[rt][f], 0, 0, 0);
   }
 
-  // The waves' parts are joined.  Register r of tile f: feature 16 f + 4
-  // quarter + r of row col.
+  // Register r of tile f: feature 16 f + 4 quarter + r of row col.
+  if constexpr (WAVES == 1) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float inv = 1.0f / over_quarters(l_run[rt], sum_of);
+      const int row = u.row0 + rt * 16 + col;
+      if (row >= u.rows) continue;
+      const bool seen = min(limit[rt], u.k1) > u.k0;
+      const int query = over(row, a.by_group);
+      uint16_t* const out = a.out + (int64_t)(u.q_beg + query) * a.ld_out + (u.kvh * G + row - query * G) * DH;
+#pragma unroll
+      for (int f = 0; f < FT; ++f) {
+        uint2 w;
+        w.x = seen ? pack_bf16x2(o[rt][f][0] * inv, o[rt][f][1] * inv) : 0u;
+        w.y = seen ? pack_bf16x2(o[rt][f][2] * inv, o[rt][f][3] * inv) : 0u;
+        *reinterpret_cast<uint2*>(out + 16 * f + 4 * quarter) = w;
+      }
+    }
+    return;
+  }
+  // The waves' parts are joined.
+  __shared__ float s_m[WAVES][RT * 16], s_l[WAVES][RT * 16];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float l = over_quarters(l_run[rt], sum_of);
@@ -877,12 +898,20 @@ __device__ __forceinline__ void tile_unit(const CacheAttention& a, const Unit& u
 template <int DH, int RT, bool SHARED>
 __global__ __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(PLACES[RT / 2][DH / 64]))) void few_rows_kernel(CacheAttention a) {
-  auto body = [&](const Unit& u) { few_rows_unit<DH, RT>(a, u); };
+  auto body = [&](const Unit& u) { few_rows_unit<DH, RT, 4>(a, u); };
   // Half of the places of 16 rows stream as much as the memory gives; a join takes as
   // long as six blocks.
   auto fit = [](int share, int most) { return most <= share * (RT == 1 ? 2 : 1) + 6; };
   if constexpr (SHARED) shared_units(a, fit, body);
-  else one_unit(a, body);
+  else one_unit(a, blockIdx.x, body);
+}
+
+// A unit a wave.
+template <int DH, int RT>
+__global__ __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(PLACES[RT / 2][DH / 64]))) void few_rows_wave_kernel(CacheAttention a) {
+  const int index = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (index < a.units) one_unit(a, index, [&](const Unit& u) { few_rows_unit<DH, RT, 1>(a, u); });
 }
 
 template <int DH, int GROUPS, bool SHARED>
@@ -891,7 +920,7 @@ __attribute__((amdgpu_waves_per_eu(SHARED ? PLACES[GROUPS / 2 + 1][DH / 64] : 2)
   auto body = [&](const Unit& u) { tile_unit<DH, GROUPS>(a, u); };
   auto fit = [](int, int) { return false; };  // (equal shares are as fast with even lengths)
   if constexpr (SHARED) shared_units(a, fit, body);
-  else one_unit(a, body);
+  else one_unit(a, blockIdx.x, body);
 }
 
 // The unit, and of a cut one the workers that have its parts, of a join.
@@ -1045,6 +1074,12 @@ __global__ __launch_bounds__(64 * WAVES) void join_kernel(CacheAttention a, int 
 template <int DH>
 hipError_t launch(const CacheAttention& a, hipStream_t stream) {
   const dim3 grid(a.workers ? a.workers : a.units), block(256);
+  if (a.wave_units) {
+    const dim3 fours((a.units + 3) / 4);
+    if (a.tile_rows == 16) hipLaunchKernelGGL((few_rows_wave_kernel<DH, 1>), fours, block, 0, stream, a);
+    else hipLaunchKernelGGL((few_rows_wave_kernel<DH, 2>), fours, block, 0, stream, a);
+    return hipGetLastError();
+  }
 #define SURGE_LAUNCH(...)                                                                  \
   do {                                                                                     \
     if (a.workers)                                                                         \
@@ -1059,9 +1094,13 @@ hipError_t launch(const CacheAttention& a, hipStream_t stream) {
 #undef SURGE_LAUNCH
   if (a.workers == 0) return hipGetLastError();
   const int rows = (int)std::min<int64_t>(a.tile_rows, (int64_t)a.max_rows * a.group);
-  if (a.workers >= 16 * a.units) {
+  // Parts that a unit is cut into, about: its rows' join has as many waves as they keep
+  // busy (by the workers alone 4 x 128 x 1500, 12 x 64 took 40 us, not 19).
+  const int blocks = ((a.c.max_length - 1) >> a.block_shift) + 1;
+  const int parts = std::min(a.workers / a.units, blocks / a.least_share);
+  if (parts >= 16) {
     hipLaunchKernelGGL((join_kernel<DH, 16, 8>), dim3(a.units * rows), dim3(1024), 0, stream, a, rows);
-  } else if (a.workers >= 4 * a.units) {
+  } else if (parts >= 4) {
     hipLaunchKernelGGL((join_kernel<DH, 4, 8>), dim3(a.units * rows), dim3(256), 0, stream, a, rows);
   } else if (a.tile_rows < 64) {
     hipLaunchKernelGGL((join_kernel<DH, 1, 4>), dim3(a.units * rows), dim3(64), 0, stream, a, rows);
@@ -1094,14 +1133,22 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
   // Sharing costs 2 us to find the shares and 5 us for the join, or 13 where tiles'
   // parts are 64 KiB each, a block 1 us (64 keys for a tile, 128 for few rows).  It is
   // left where units are short or fill the chip twice over.  Measured, a unit a
-  // workgroup / shared, us: 1 x 1000 queries x 1000 keys, 16 / 4 x 128 27 / 56; 200 x 4
-  // x 500, 12 x 64 23 / 45; 8 x 2048 x 8192, 16 x 128 1047 / 1144; 1 x 512 x 30,000,
-  // 16 / 4 x 128 400 / 146; 48 x 1 x about 8000, 32 / 8 x 128 96 / 87.
+  // workgroup / shared, us:
+  //   30 x 1 x 800, 16 / 4 x 128 10 / 12; 200 x 4 x 500, 12 x 64 23 / 45; 48 x 1 x about
+  //   8000, 32 / 8 x 128 96 / 87
+  //   (few tiles) 10 x 12 x 1100, 32 / 8 x 128 23 / 18; 1 x 128 x 2000, 8 x 128 47 / 23
+  //   (more) 34 x 148 x 1938, 12 x 64 61 / 77; 8 x 2048 x 8192, 16 x 128 1047 / 1144
   s.least_share = cls >= 2 ? 8 : 2;
   s.workers = 0;
-  if (most > (cls >= 2 ? 32 : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) &&
+  if (most > (cls >= 2 ? (s.units <= workers / 4 ? 16 : 32) : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) &&
       s.units <= (cls >= 2 ? 2 : 1) * workers)
     s.workers = workers;
+  // Where units of few rows are short or very many, a wave has one for itself: no waves
+  // without keys and no join of four.  Measured, a workgroup / a wave, us: 400 x 1 x 60,
+  // 32 / 8 x 128 17.0 / 11.0; 200 x 8 x 100, 16 / 4 x 128 15.0 / 10.7; 1000 x 8 x 240, 32 / 8 x
+  // 128 111 / 93; but 140 x 1 x 240 12.5 / 14.1 and 400 x 1 x 900 79 / 90.
+  s.wave_units =
+      cls < 2 && s.workers == 0 && s.units > workers && (max_length <= 128 || s.units >= 8 * workers);
   return s;
 }
 

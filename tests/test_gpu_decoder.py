@@ -449,6 +449,40 @@ def test_attention_of_marked_keys(lengths, rows, heads, hk, dh, which):
     assert nan[:rows[0], (hk - 1) * G * dh:].all() and int(nan.sum()) == rows[0] * G * dh
 
 
+# Many units, of a few rows each and short, or so many that each is a wave's.
+MANY = [(500, 1, 100, 16, 4, 4, 32), (400, 6, 128, 32, 16, 4, 32), (300, 1, 90, 16, 8, 4, 64), (300, 7, 60, 64, 12, 3, 64),
+        (200, 1, 33, 16, 32, 8, 128), (150, 5, 128, 32, 16, 4, 128), (800, 1, 230, 32, 8, 8, 128),
+        (520, 17, 300, 16, 8, 8, 128)]
+
+
+@pytest.mark.parametrize("seqs,rows,length,page,heads,hk,dh", MANY)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_many_units(seqs, rows, length, page, heads, hk, dh, causal):
+    """And with a page that is missing, which some rows of one sequence see."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(seqs + rows)
+    lengths = rng.integers(0, length, seqs)
+    lengths[seqs // 2] = length
+    counts = rng.integers(0, rows + 1, seqs)
+    counts[seqs // 2] = rows
+    counts = [int(r) for r in counts]
+    c = Cache(lengths, page, hk, dh, seqs).fill(2)
+    n, w = sum(counts), heads * dh
+    q, _ = strided(randn(gen(3), n, w).bfloat16(), 8)
+    ref, tol = reference(c, q, counts, heads, causal)
+    out = torch.full((n + 2, w + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert attend(c, q, counts, heads, causal, out) == 0  # not shared out
+    within(out[:n, :w], ref, tol)
+    assert (out[n:] == 7).all() and (out[:, w:] == 7).all()
+    i, entry = seqs // 2, (length - 1) // page
+    c.table[i, entry] = -1
+    at = sum(counts[:i])
+    sees = [at + j for j in range(rows) if not causal or length - rows + j >= entry * page]
+    ref[sees] = math.nan
+    attend(c, q, counts, heads, causal, out)
+    agrees(out[:n, :w], ref, tol)
+
+
 @pytest.mark.parametrize("lengths,rows,heads,hk,dh", SHAPES)
 def test_attention_of_missing_pages_and_nan_queries(lengths, rows, heads, hk, dh):
     torch = torch_cuda()
