@@ -12,7 +12,7 @@
 // bf16 for their product with V, not in their sum.  S^T = K Q^T and O^T += V^T P^T,
 // so that a lane owns a row's maximum, sum and rescaling and the probabilities are
 // the second product's operand where they are.  Three arrangements, by the rows of a
-// (sequence, key head) in the call:
+// (sequence, key head) in the call (and see cache_attention_shape):
 //
 // Up to 16 or 32 rows (a step, drafts): waves with blocks of 32 keys of their own
 // against all rows in 16x16x32 MFMAs.  A lane loads a quarter of a key, whose codes
@@ -547,20 +547,27 @@ __device__ __forceinline__ void few_rows_unit(const CacheAttention& a, const Uni
 
   // Register r of tile f: feature 16 f + 4 quarter + r of row col.
   if constexpr (WAVES == 1) {
+    // Through LDS, so that whole rows are stored, 16 bytes a lane.
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       const float inv = 1.0f / over_quarters(l_run[rt], sum_of);
-      const int row = u.row0 + rt * 16 + col;
-      if (row >= u.rows) continue;
       const bool seen = min(limit[rt], u.k1) > u.k0;
-      const int query = over(row, a.by_group);
-      uint16_t* const out = a.out + (int64_t)(u.q_beg + query) * a.ld_out + (u.kvh * G + row - query * G) * DH;
 #pragma unroll
       for (int f = 0; f < FT; ++f) {
         uint2 w;
         w.x = seen ? pack_bf16x2(o[rt][f][0] * inv, o[rt][f][1] * inv) : 0u;
         w.y = seen ? pack_bf16x2(o[rt][f][2] * inv, o[rt][f][3] * inv) : 0u;
-        *reinterpret_cast<uint2*>(out + 16 * f + 4 * quarter) = w;
+        reinterpret_cast<uint2*>(sv + v_slot<CPR>(16 * rt + col, 2 * f + (quarter >> 1)))[quarter & 1] = w;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < RT * CPR / 4; ++j) {
+      const int r = j * (64 / CPR) + lane / CPR, chunk = lane % CPR, row = u.row0 + r;
+      const u32x4 w = sv[v_slot<CPR>(r, chunk)];
+      if (row < u.rows) {
+        const int query = over(row, a.by_group);
+        *reinterpret_cast<u32x4*>(a.out + (int64_t)(u.q_beg + query) * a.ld_out + (u.kvh * G + row - query * G) * DH +
+                                  chunk * 8) = w;
       }
     }
     return;
@@ -1123,12 +1130,22 @@ CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_head
                                  int64_t max_length, int n_cus) {
   CacheShape s;
   const int64_t rows = max_rows * group;
-  const int cls = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+  const auto workers_of = [&](int cls) { return (int64_t)n_cus * PLACES[cls][d_head / 64] / 8 * 8; };
+  int cls = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+  // Against up to 96 keys up to 64 rows, or rows that leave a quarter of their tiles empty,
+  // are many waves' units of 32 rows, where those fill the chip: a tile's few blocks don't
+  // pay its barriers.  Measured, a tile / waves, us: 841 x 15 x 15, 16 / 4 x 128 43 / 31; 400 x
+  // 50 x 64, 16 x 64 32.7 / 27.9; 4000 x about 48 x 48, 12 x 64 257 / 190; 116 x 37 x 37, 32 /
+  // 8 x 128 24.5 / 20.8; but 423 x 30 x 30 50 / 55 and 200 x 128 x 128, 12 x 64 23.3 / 26.8.
+  const int64_t pieces = (rows + 31) / 32;
+  if (cls >= 2 && max_length <= 96 && (cls == 2 || pieces <= 3 * ((rows + 127) / 128)) &&
+      n_seqs * n_kv_heads * pieces > workers_of(1))
+    cls = 1;
   s.tile_rows = 16 << cls;
   s.block_shift = cls >= 2 ? 6 : 7;  // few rows: 32 keys for each of four waves
   s.tiles = (rows + s.tile_rows - 1) / s.tile_rows;
   s.units = n_seqs * n_kv_heads * s.tiles;
-  const int64_t workers = (int64_t)n_cus * PLACES[cls][d_head / 64] / 8 * 8;
+  const int64_t workers = workers_of(cls);
   const int64_t most = ((max_length - 1) >> s.block_shift) + 1;  // blocks of a unit
   // Sharing costs 2 us to find the shares and 5 us for the join, or 13 where tiles'
   // parts are 64 KiB each, a block 1 us (64 keys for a tile, 128 for few rows).  It is

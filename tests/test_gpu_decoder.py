@@ -452,7 +452,8 @@ def test_attention_of_marked_keys(lengths, rows, heads, hk, dh, which):
 # Many units, of a few rows each and short, or so many that each is a wave's.
 MANY = [(500, 1, 100, 16, 4, 4, 32), (400, 6, 128, 32, 16, 4, 32), (300, 1, 90, 16, 8, 4, 64), (300, 7, 60, 64, 12, 3, 64),
         (200, 1, 33, 16, 32, 8, 128), (150, 5, 128, 32, 16, 4, 128), (800, 1, 230, 32, 8, 8, 128),
-        (520, 17, 300, 16, 8, 8, 128)]
+        (520, 17, 300, 16, 8, 8, 128), (400, 50, 64, 16, 4, 4, 64), (150, 90, 96, 16, 2, 2, 128), (60, 148, 90, 32, 2, 2, 128),
+        (300, 20, 70, 32, 12, 3, 32)]
 
 
 @pytest.mark.parametrize("seqs,rows,length,page,heads,hk,dh", MANY)
