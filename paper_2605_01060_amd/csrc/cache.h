@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "cache_shape.h"
+
 namespace surge {
 
 // Pages of tokens, see surge_kv_cache.  A page holds for every key head, in
@@ -53,8 +55,8 @@ struct CacheAttention {
   int group, max_rows;
   bool causal;
   float scale_log2;   // scale * log2(e)
-  // Of cache_attention_shape.
-  int tile_rows, block_shift, tiles, units, workers, least_share;
+  // Of cache_attention_shape, and of cache_attention_join.
+  int tile_rows, block_shift, tiles, units, workers, least_share, join_waves;
   bool wave_units;
   Divisor by_group, by_tiles, by_heads, by_units, by_workers;  // by_units: by n_seqs * n_kv_heads
   // Workspace, where there are workers: of the two slots that each has for the
@@ -65,21 +67,6 @@ struct CacheAttention {
   int2* joins;       // [unit] first and last worker; first < 0: not cut
 };
 
-// How a call is cut into units: tiles of tile_rows rows (query * group + head
-// of the group) of each (sequence, key head).  Their keys, in blocks of
-// 1 << block_shift, are shared out to `workers` workgroups, at least least_share blocks
-// each, or where that is 0 a unit is a workgroup's.
-struct CacheShape {
-  int tile_rows, block_shift, least_share;
-  bool wave_units;  // a unit is a wave's
-  int64_t tiles, units, workers;
-  int64_t slot_rows() const { return 2 * workers * tile_rows; }
-  int64_t workspace_bytes(int d_head) const {
-    return workers ? slot_rows() * (8 + 4 * (int64_t)d_head) + units * 8 : 0;
-  }
-};
-CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_kv_heads, int group, int d_head,
-                                 int64_t max_length, int n_cus);
 hipError_t launch_cache_attention(const CacheAttention& a, int d_head, hipStream_t stream);
 
 struct VerifyDrafts {

@@ -228,6 +228,7 @@ surge_status surge_op_cache_attention(const surge_kv_cache* cache, int64_t n_row
   a.by_units = divisor(cache->n_seqs * cache->n_kv_heads);
   a.by_workers = divisor(std::max(a.workers, 1));
   a.least_share = s.least_share;
+  a.join_waves = s.workers ? cache_attention_join(s, cache->max_length) : 0;
   a.wave_units = s.wave_units;
   a.part_o = (float*)d_workspace;
   a.part_ml = (float2*)(a.part_o + s.slot_rows() * cache->d_head);

@@ -397,6 +397,48 @@ def test_attention_of_batches(seqs, rows, length, page, heads, hk, dh, causal):
     check(c, [int(r) for r in counts], heads, causal, 3)
 
 
+# Every arrangement of units that are shared out, for each kind of tile and size of
+# heads (tests/test_cache_shapes.py states which a call takes): sequences, rows,
+# shortest and longest length, page, heads.
+SHARED = [
+    # 16 and 32 rows: whole units (even lengths), equal shares, equal parts.
+    (64, 4, 1200, 1500, 32, 32, 8, 128), (130, 4, 1200, 1500, 64, 16, 4, 64), (150, 8, 1200, 1500, 16, 6, 3, 32),
+    (64, 8, 1250, 1500, 32, 32, 8, 128), (130, 7, 1250, 1500, 64, 16, 4, 64), (400, 10, 1250, 1500, 128, 6, 2, 32),
+    (50, 3, 0, 4000, 16, 20, 4, 128), (70, 16, 0, 3000, 64, 4, 4, 64), (45, 5, 0, 3500, 32, 33, 11, 32),
+    (40, 20, 0, 3100, 32, 4, 4, 128), (60, 9, 0, 2500, 64, 12, 4, 64), (50, 16, 0, 2700, 16, 16, 8, 32),
+    (6, 1, 0, 3001, 16, 16, 2, 64), (6, 31, 0, 3001, 64, 2, 2, 128), (9, 17, 0, 2500, 16, 6, 6, 32),
+    # 64 and 128 rows: equal shares, several units a workgroup; equal parts.
+    (64, 16, 0, 2300, 64, 16, 4, 128), (20, 60, 0, 2400, 32, 16, 16, 64), (30, 30, 0, 2500, 16, 24, 12, 32),
+    (5, 50, 0, 2300, 64, 4, 4, 128), (7, 16, 0, 2200, 64, 12, 3, 64), (6, 64, 0, 2100, 32, 4, 4, 32),
+    (20, 70, 0, 2300, 64, 16, 8, 128), (9, 300, 0, 2400, 32, 16, 8, 64), (16, 200, 0, 2500, 16, 9, 9, 32),
+    # Threads whose (sequence, tile) pairs begin inside a sequence.
+    (5, 1000, 1000, 2600, 64, 8, 1, 128), (9, 900, 0, 2500, 32, 4, 1, 64), (3, 2000, 2000, 2700, 32, 6, 1, 32),
+]
+
+
+def shared_call(seqs, rows, shortest, length):
+    """Lengths and rows of a call of SHARED: some sequences without keys, some
+    without rows, the longest in the middle with the most rows."""
+    rng = np.random.default_rng(seqs * rows)
+    lengths = rng.integers(shortest, length + 1, seqs)
+    lengths[rng.random(seqs) < 0.1] = 0
+    counts = rng.integers(max(rows // 2, 1), rows + 1, seqs)
+    counts[rng.random(seqs) < 0.1] = 0
+    lengths[seqs // 2], counts[seqs // 2] = length, rows
+    return lengths, [int(r) for r in counts]
+
+
+@pytest.mark.parametrize("seqs,rows,shortest,length,page,heads,hk,dh", SHARED)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_shared_units(seqs, rows, shortest, length, page, heads, hk, dh, causal):
+    torch = torch_cuda()
+    lengths, counts = shared_call(seqs, rows, shortest, length)
+    c = Cache(lengths, page, hk, dh, seqs).fill(2)
+    need, out = check(c, counts, heads, causal, 3)
+    assert need > 0
+    assert torch.equal(out, check(c, counts, heads, causal, 3)[1])
+
+
 def test_attention_of_prompts_without_a_cache_before():
     """Rows for every position of sequences, one tile and more."""
     lengths = [130, 64, 1, 257, 640]
