@@ -779,6 +779,46 @@ def test_verify_at_the_edges():
     assert got[0][3, 0] == -1 and got[0][13, 0] == -1
 
 
+@pytest.mark.parametrize("vocab,pad", [(5000, 0), (40_001, 3), (100_003, 0), (300_007, 1)])
+def test_verify_at_the_edges_of_large_vocabularies(vocab, pad):
+    """One launch and two, more tiles than a wave has lanes: what leaves nothing
+    over, is not finite or nothing at all, tokens in the first and last tile."""
+    torch = torch_cuda()
+    n, k = 18, 2
+    p, q, drafts, u = draft_inputs(n, k, vocab, 1)
+    drafts[0, 0], drafts[1, 0], drafts[2, 1] = -1, vocab, 1 << 30
+    p[3] = 0                                     # nothing to draw: -1
+    p[4, 0, vocab - 7] = math.inf                # infinite: -1
+    drafts[4, 0], u[4, 0] = 3, 0.999999
+    p[5, :, ::2] = math.nan                      # counts as 0
+    p[6, 0], u[6, 0] = q[6, 0], 2.0              # nothing left over: the target's own
+    u[7] = 0.0
+    u[8] = 1 - 2.0 ** -24
+    p[9, :, vocab - 900:], u[9, k] = 0, 2.0      # beyond every sum: the last that weighs anything
+    u[10] = math.nan
+    q[11] = math.nan
+    p[12, :, :4500], u[12, k] = 0, 0.0           # the first tokens weigh nothing
+    p[13] = -p[13]
+    p[14, 0], drafts[14, 0], u[14, 0] = 0, vocab - 1, 2.0
+    p[14, 0, vocab - 1] = 1                      # a draft with all of the target's mass, rejected
+    q[14, 0] = p[14, 0]
+    p[15, 0], u[15, 0] = q[15, 0], 2.0
+    p[15, 0, vocab // 2] += 2.0 ** -10           # one token left over
+    q[16], u[16] = 1.0, 0.999                    # less than q everywhere
+    p[17, 0], p[17, 0, 5], u[17, 0] = 0, math.inf, 2.0
+    q[17, 0], drafts[17, 0] = math.inf, 5        # inf - inf: the target's own, infinite: -1
+    counts = np.full(n, k)
+    for x in (q, None):
+        want = verified(p, x, drafts, counts, u)
+        got = verify(p, x, drafts, counts, u, pad=pad)
+        assert np.array_equal(got[0], want[0]), (got[0], want[0])
+        assert np.array_equal(got[1], want[1])
+        assert (got[0][[3, 13], 0] == -1).all() and got[0][14, 0] == vocab - 1
+        again = verify(p, x, drafts, counts, u, pad=pad)
+        assert np.array_equal(got[0], again[0])
+    assert verified(p, q, drafts, counts, u)[0][15, 0] == vocab // 2
+
+
 def test_verify_takes_the_token_on_either_side_of_a_border():
     """Sums that are exact: u at a border takes the next token."""
     torch = torch_cuda()
