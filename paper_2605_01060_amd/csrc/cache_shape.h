@@ -60,12 +60,15 @@ inline CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_
   if (most > (cls >= 2 ? (s.units <= workers / 4 ? 16 : 32) : 8) && n_seqs * s.tiles <= 2048 && s.units * most < (1 << 30) &&
       s.units <= (cls >= 2 ? 2 : 1) * workers)
     s.workers = workers;
-  // Where units of few rows are short or very many, a wave has one for itself: no waves
-  // without keys and no join of four.  Measured, a workgroup / a wave, us: 400 x 1 x 60,
-  // 32 / 8 x 128 17.0 / 11.0; 200 x 8 x 100, 16 / 4 x 128 15.0 / 10.7; 1000 x 8 x 240, 32 / 8 x
-  // 128 111 / 93; but 140 x 1 x 240 12.5 / 14.1 and 400 x 1 x 900 79 / 90.
-  s.wave_units =
-      cls < 2 && s.workers == 0 && s.units > workers && (max_length <= 128 || s.units >= 8 * workers);
+  // Where units of few rows are short, or very many and not long, a wave has one for
+  // itself: no waves without keys and no join of four.  Measured, a workgroup / a wave, us:
+  // 400 x 1 x 60, 32 / 8 x 128 17.0 / 11.0; 200 x 8 x 100, 16 / 4 x 128 15.0 / 10.7; 1000 x 8 x
+  // 240, 32 / 8 x 128 109 / 88, 1000 x 8 x 1024 286 / 251, 800 x 1 x 1024 161 / 174; but 140 x 1
+  // x 240 12.5 / 14.1 and 400 x 1 x 900 79 / 90.  max_length says nothing of most sequences,
+  // but one may be as long, and the call then waits for its wave: among 800 x 1 of about 200
+  // keys, 32 / 8 x 128, one of 1024 43 / 40, of 2048 43 / 66, of 30,000 212 / 773.
+  s.wave_units = cls < 2 && s.workers == 0 && s.units > workers &&
+                 (max_length <= 128 || (max_length <= 1024 && s.units >= 8 * workers));
   return s;
 }
 

@@ -147,3 +147,23 @@ def test_calls_of_many_units(shape, call):
     seqs, rows, length, _, heads, hk, dh = call
     tile, who, *_ = taken(shape, *many_call(seqs, rows, length), heads, hk, dh)
     assert (tile < 64) == (who == "wave")
+
+
+@pytest.mark.parametrize("rows,hk,group,dh", [(1, 8, 4, 128), (8, 8, 4, 128), (1, 12, 1, 64), (30, 8, 1, 64),
+                                              (1, 12, 1, 32), (20, 12, 1, 32)])
+def test_no_wave_has_a_long_unit_to_itself(shape, rows, hk, group, dh):
+    """One sequence's keys may be as many as max_length says, however short the
+    others are: beyond 1024 a unit has a workgroup, however many units there are."""
+    for seqs in (2000, 20_000):
+        for length in (1025, 2048, 8192, 100_003, 1 << 30):
+            assert not shape(seqs, rows, hk, group, dh, length)["wave_units"], (seqs, length)
+        for length in (1, 128, 240, 1024):
+            assert shape(seqs, rows, hk, group, dh, length)["wave_units"], (seqs, length)
+
+
+@pytest.mark.parametrize("seqs,rows,longest,page,heads,hk,dh", D.TAILS)
+def test_calls_of_one_long_sequence_among_many(shape, seqs, rows, longest, page, heads, hk, dh):
+    s = shape(seqs, rows, hk, heads // hk, dh, longest)
+    places = {16: {32: 7, 64: 4, 128: 3}, 32: {32: 5, 64: 3, 128: 2}}[s["tile_rows"]][dh]
+    assert s["units"] >= 8 * CUS * places
+    assert s["workers"] == 0 and s["wave_units"] == (longest <= 1024)

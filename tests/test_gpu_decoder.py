@@ -439,6 +439,21 @@ def test_attention_of_shared_units(seqs, rows, shortest, length, page, heads, hk
     assert torch.equal(out, check(c, counts, heads, causal, 3)[1])
 
 
+# One long sequence, the last, among very many short ones: a wave has a unit up to 1024
+# keys, a workgroup beyond.
+TAILS = [(800, 1, 1024, 16, 16, 8, 128), (800, 1, 1025, 16, 16, 8, 128), (800, 3, 9001, 64, 16, 8, 128),
+         (700, 1, 1024, 32, 12, 12, 64), (700, 16, 5003, 32, 12, 12, 64), (1200, 2, 1000, 16, 24, 12, 32),
+         (1200, 1, 20_011, 128, 12, 12, 32), (900, 8, 1024, 16, 32, 8, 128), (900, 7, 3001, 64, 32, 8, 128)]
+
+
+@pytest.mark.parametrize("seqs,rows,longest,page,heads,hk,dh", TAILS)
+def test_attention_of_one_long_sequence_among_many(seqs, rows, longest, page, heads, hk, dh):
+    lengths = np.random.default_rng(seqs + rows).integers(0, 70, seqs)
+    lengths[-1] = longest
+    c = Cache(lengths, page, hk, dh, seqs).fill(2)
+    check(c, [rows] * seqs, heads, True, 3)
+
+
 def test_attention_of_prompts_without_a_cache_before():
     """Rows for every position of sequences, one tile and more."""
     lengths = [130, 64, 1, 257, 640]
