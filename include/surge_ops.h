@@ -289,7 +289,11 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
  *
  * d_pages 16-byte aligned; n_pages below 2^31; n_kv_heads at most 1024; n_seqs
  * at most 2^20; ld_table at least max_length / page_tokens, rounded up;
- * max_length and n_rows at most 2^30.  The struct is read by the call.
+ * max_length and n_rows at most 2^30.  The struct is read by the call.  A call that
+ * needs a larger grid than a launch has is refused with SURGE_ERR_CAPACITY: a write or
+ * read of more than 2^29 rows, counted for each four key heads, attention of more than
+ * 2^23 units, a unit being 128 rows (query x heads of the group; 16, 32 or 64 where a
+ * sequence has no more) of a sequence and key head.
  */
 typedef struct surge_kv_cache {
   uint8_t* d_pages;

@@ -36,6 +36,7 @@ struct CacheStore {
   int64_t ld_k, ld_v;
   int heads_each;  // of a wave: the launch's
 };
+int64_t cache_store_blocks(int64_t n_rows, int n_kv_heads, int d_head);  // of 256 threads, of a launch
 hipError_t launch_cache_write(CacheStore a, int d_head, hipStream_t stream);
 hipError_t launch_cache_read(CacheStore a, int d_head, hipStream_t stream);
 

@@ -17,7 +17,7 @@ constexpr int64_t kMostLength = 1 << 30;
 constexpr int kMaxSeqs = 1 << 20, kMaxHeads = 1024, kMaxDrafts = 1024;
 constexpr int kMaxVocab = 1 << 22;
 // Threads of a launch are a 32-bit number.
-constexpr int64_t kMostThreads = INT32_MAX;
+constexpr int64_t kMostThreads = 1ll << 31;
 
 int64_t head_bytes(const surge_kv_cache* c) {
   return (int64_t)c->page_tokens * c->d_head / 16 * 17;
@@ -101,7 +101,7 @@ surge_status store(bool write, const surge_kv_cache* cache, int64_t n_rows, cons
   if (d_k == d_v && !write) return fail(SURGE_ERR_INVALID_ARGUMENT, "k is v");
   if ((const void*)d_k == cache->d_pages || (const void*)d_v == cache->d_pages)
     return fail(SURGE_ERR_INVALID_ARGUMENT, "k or v is pages");
-  if ((n_rows + 15) / 16 * cache->n_kv_heads * 64 > kMostThreads - 255)
+  if (cache_store_blocks(n_rows, cache->n_kv_heads, cache->d_head) > kMostThreads / 256)
     return fail(SURGE_ERR_CAPACITY, "too many rows and heads for one call");
   int dev = 0, n_cus = 0;
   CHECK(current_device((hipStream_t)hip_stream, &dev, &n_cus));
@@ -117,8 +117,8 @@ surge_status attention_shape(const surge_kv_cache* c, int64_t max_rows, int32_t 
                              CacheShape* s, int64_t* bytes) {
   *s = cache_attention_shape(c->n_seqs, max_rows, c->n_kv_heads, n_heads / c->n_kv_heads, c->d_head,
                              c->max_length, n_cus);
-  // Threads of the units' launch and, where they are joined, of a wave a row.
-  if (s->units > kMostThreads / 256 || (s->workers && s->units * s->tile_rows > kMostThreads / 64))
+  // (Units that are shared out, and with them the rows of their join, are few.)
+  if ((s->wave_units ? (s->units + 3) / 4 : s->units) > kMostThreads / 256)
     return fail(SURGE_ERR_CAPACITY, "too many rows, heads and sequences for one call");
   *bytes = s->workspace_bytes(c->d_head);
   return SURGE_OK;

@@ -246,20 +246,21 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheStore a) {
 
 // Heads of a wave: one step's in small calls, which need the waves, four in large ones,
 // whose waves find their rows' places once for them.
-int heads_each(const CacheStore& a, int d_head) {
-  const int64_t waves = ((int64_t)a.r.n_rows + ROWS - 1) / ROWS * a.c.n_kv_heads;
+int heads_each(int64_t n_rows, int n_kv_heads, int d_head) {
+  const int64_t waves = (n_rows + ROWS - 1) / ROWS * n_kv_heads;
   return waves > FEW_WAVES ? 4 : d_head < 64 ? 64 / d_head : 1;
-}
-unsigned blocks(const CacheStore& a) {
-  const int64_t groups = (a.c.n_kv_heads + a.heads_each - 1) / a.heads_each;
-  return (unsigned)((((int64_t)a.r.n_rows + ROWS - 1) / ROWS * groups + 31) / 32 * 8);
 }
 
 }  // namespace
 
+int64_t cache_store_blocks(int64_t n_rows, int n_kv_heads, int d_head) {
+  const int each = heads_each(n_rows, n_kv_heads, d_head);
+  return ((n_rows + ROWS - 1) / ROWS * ((n_kv_heads + each - 1) / each) + 31) / 32 * 8;
+}
+
 hipError_t launch_cache_write(CacheStore a, int d_head, hipStream_t stream) {
-  a.heads_each = heads_each(a, d_head);
-  const dim3 grid(blocks(a));
+  a.heads_each = heads_each(a.r.n_rows, a.c.n_kv_heads, d_head);
+  const dim3 grid((unsigned)cache_store_blocks(a.r.n_rows, a.c.n_kv_heads, d_head));
   if (d_head == 32) hipLaunchKernelGGL(cache_write_kernel<32>, grid, dim3(256), 0, stream, a);
   if (d_head == 64) hipLaunchKernelGGL(cache_write_kernel<64>, grid, dim3(256), 0, stream, a);
   if (d_head == 128) hipLaunchKernelGGL(cache_write_kernel<128>, grid, dim3(256), 0, stream, a);
@@ -267,8 +268,8 @@ hipError_t launch_cache_write(CacheStore a, int d_head, hipStream_t stream) {
 }
 
 hipError_t launch_cache_read(CacheStore a, int d_head, hipStream_t stream) {
-  a.heads_each = heads_each(a, d_head);
-  const dim3 grid(blocks(a));
+  a.heads_each = heads_each(a.r.n_rows, a.c.n_kv_heads, d_head);
+  const dim3 grid((unsigned)cache_store_blocks(a.r.n_rows, a.c.n_kv_heads, d_head));
   if (d_head == 32) hipLaunchKernelGGL(cache_read_kernel<32>, grid, dim3(256), 0, stream, a);
   if (d_head == 64) hipLaunchKernelGGL(cache_read_kernel<64>, grid, dim3(256), 0, stream, a);
   if (d_head == 128) hipLaunchKernelGGL(cache_read_kernel<128>, grid, dim3(256), 0, stream, a);

@@ -914,6 +914,44 @@ def test_attention_of_a_hundred_thousand_sequences():
     assert torch.equal(out.double().view(n, hk, 2, dh), held.view(n, hk, 1, dh).expand(n, hk, 2, dh))
 
 
+def test_attention_of_a_million_sequences():
+    """2^20 sequences of 8 key heads, as many as a call takes: a wave each."""
+    torch = torch_cuda()
+    n, hk, dh = 1 << 20, 8, 32
+    lengths = np.random.default_rng(1).integers(0, 2, n)
+    c = Cache(lengths, 16, hk, dh, 1)
+    g = gen(1)
+    k, v, q = (torch.randn(n, hk * dh, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    S.surge_op_cache_write(c.desc, n, None, k, hk * dh, v, hk * dh)
+    out = torch.empty_like(q)
+    attend(c, q, [1] * n, hk, True, out)
+    on = torch.from_numpy(lengths).cuda()
+    for i in range(0, n, 1 << 17):
+        at = slice(i, i + (1 << 17))
+        assert torch.equal(out[at].double(), values(*quantized(v[at])) * on[at, None])
+
+
+@pytest.mark.parametrize("n,hk", [((1 << 27) + 1024, 4), (1 << 29, 1)])
+def test_rows_that_need_a_launch_of_the_largest_size(n, hk):
+    """More than 2^29 rows times key heads, a wave's four heads together, and 2^29
+    rows of one: rows of negative positions but for the last ones."""
+    torch = torch_cuda()
+    dh, m = 32, 40
+    w = hk * dh
+    x = torch.empty(n, 2 * w, dtype=torch.bfloat16, device="cuda")
+    last = randn(gen(1), m, 2 * w).bfloat16()
+    x[-m:] = last
+    c = Cache([m], 16, hk, dh, 1, fill=0xAB)
+    want = c.pages.clone()
+    c.put(0, np.arange(m), last[:, :w], last[:, w:], want)
+    S.surge_op_cache_write(c.desc, n, None, x, 2 * w, x[:, w:], 2 * w)
+    assert torch.equal(c.pages, want)
+    x[::1 << 20] = 7.0
+    S.surge_op_cache_read(c.desc, n, None, x, 2 * w, x[:, w:], 2 * w)
+    assert torch.equal(x[-m:].double(), values(*quantized(last)))
+    assert not x[:-m].view(torch.int16)[::1 << 10].any() and not x[:-m][::1 << 20].any()
+
+
 @pytest.mark.parametrize("rows", [[2, 3], [60, 70]])
 def test_attention_with_pages_shared_by_sequences(rows):
     """Two sequences that begin alike, with the same pages."""
