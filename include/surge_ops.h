@@ -347,7 +347,9 @@ surge_status surge_op_cache_read(const surge_kv_cache* cache, int64_t n_rows, co
  * 2^127.  max_length and max_rows cut the call into units, so in a captured
  * call they are the bounds of its replays.  d_workspace as in cross attention,
  * of surge_cache_attention_workspace bytes for the same cache, max_rows and
- * n_heads.  d_out must not overlap an input.
+ * n_heads: more sequences, rows or keys may need less, so a program whose calls
+ * differ in them asks for each and keeps the largest, at most 68.2 MB on 256
+ * compute units.  d_out must not overlap an input.
  */
 surge_status surge_cache_attention_workspace(const surge_kv_cache* cache, int64_t max_rows,
                                              int32_t n_heads, int64_t* bytes);

@@ -510,7 +510,8 @@ def surge_op_cache_read(cache: KVCache, n_rows, d_cu, d_k, ld_k, d_v, ld_v, stre
 
 
 def surge_cache_attention_workspace(cache: KVCache, max_rows: int, n_heads: int) -> int:
-    """Bytes of workspace that a call needs on the current device."""
+    """Bytes of workspace that a call needs on the current device (not always more
+    for more sequences, rows or keys: the largest of a program's calls' serves all)."""
     v = ctypes.c_int64(0)
     _check(lib().surge_cache_attention_workspace(ctypes.byref(cache), max_rows, n_heads,
                                                  ctypes.byref(v)))

@@ -19,7 +19,7 @@ extern "C" void shape(int64_t n_seqs, int64_t max_rows, int hk, int group, int d
   const CacheShape s = cache_attention_shape(n_seqs, max_rows, hk, group, dh, max_length, cus);
   out[0] = s.tile_rows, out[1] = s.block_shift, out[2] = s.tiles, out[3] = s.units, out[4] = s.workers;
   out[5] = s.least_share, out[6] = s.wave_units;
-  out[7] = s.workers ? cache_attention_join(s, max_length) : -1;
+  out[7] = s.workers ? cache_attention_join(s, max_length) : -1, out[8] = s.workspace_bytes(dh);
 }
 """
 
@@ -35,9 +35,10 @@ def shape(tmp_path_factory):
     lib.shape.argtypes = [ctypes.c_int64] * 2 + [ctypes.c_int] * 3 + [ctypes.c_int64, ctypes.c_int, ctypes.c_void_p]
 
     def of(n_seqs, max_rows, hk, group, dh, max_length):
-        out = np.zeros(8, np.int64)
+        out = np.zeros(9, np.int64)
         lib.shape(n_seqs, max_rows, hk, group, dh, max_length, CUS, out.ctypes.data)
-        names = ("tile_rows", "block_shift", "tiles", "units", "workers", "least_share", "wave_units", "join")
+        names = ("tile_rows", "block_shift", "tiles", "units", "workers", "least_share", "wave_units", "join",
+                 "workspace")
         return dict(zip(names, out.tolist()))
 
     return of
@@ -167,3 +168,17 @@ def test_calls_of_one_long_sequence_among_many(shape, seqs, rows, longest, page,
     places = {16: {32: 7, 64: 4, 128: 3}, 32: {32: 5, 64: 3, 128: 2}}[s["tile_rows"]][dh]
     assert s["units"] >= 8 * CUS * places
     assert s["workers"] == 0 and s["wave_units"] == (longest <= 1024)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_workspaces_stay_within_what_is_documented(shape, dh):
+    most = 0
+    for seqs in (1, 2, 5, 16, 48, 64, 96, 97, 128, 192, 256, 500, 700, 1000, 2048):
+        for hk in (1, 2, 4, 8, 12, 64):
+            for rows in (1, 4, 8, 16, 60, 128, 500, 5000, 1 << 20):
+                for length in (100, 900, 1100, 2000, 3000, 100_003, 1 << 30):
+                    most = max(most, shape(seqs, rows, hk, 4, dh, length)["workspace"])
+    assert 0 < most <= 68_200_000
+    # More sequences may need less: 96 of 8 key heads are shared out, 97 are not.
+    if dh == 128:
+        assert shape(96, 1, 8, 4, dh, 8000)["workspace"] > 0 == shape(97, 1, 8, 4, dh, 8000)["workspace"]
