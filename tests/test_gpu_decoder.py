@@ -13,7 +13,8 @@ import pytest
 
 from gpu_util import torch_cuda
 from paper_2605_01060_amd import surge as S
-from test_gpu_reader import BF16, F32, gen, randn, strided, within
+from test_gpu_reader import (BF16, EPS, F32, check_i8, gen, linear_reference, norm_reference, quantized32, randn,
+                             strided, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -1106,3 +1107,126 @@ def test_decoder_steps_captured_and_replayed():
     torch.cuda.synchronize()
     for r in replayed:
         assert torch.equal(r.out, r.want)
+
+
+class Block:
+    """A decoder's block of the library's operators alone: n = RMS(x) in int8;
+    Q | K | V = n W in one matrix; K and V's columns to the cache; A = attention of
+    Q's columns; y = x + A Wo."""
+
+    def __init__(self, lengths, d, page, heads, hk, dh, seed):
+        torch = torch_cuda()
+        self.d, self.heads, self.c = d, heads, Cache(lengths, page, hk, dh, seed, room=200).fill(seed)
+        g, self.wide = gen(seed), (heads + 2 * hk) * dh
+        self.w, self.ws, self.bias = {}, {}, {}
+        for name, n, k in (("qkv", self.wide, d), ("o", d, heads * dh)):
+            q, s = quantized32(randn(g, n, k) / math.sqrt(k))
+            self.w[name], self.ws[name], self.bias[name] = q.cuda(), s.contiguous().cuda(), 0.1 * randn(g, n)
+        self.gamma = 1 + 0.1 * randn(g, d)
+
+    def rows(self, rows, seed):
+        """Room and inputs for a call of these rows."""
+        torch = torch_cuda()
+        c, m, qd = self.c, sum(rows), self.heads * self.c.dh
+        self.given, self.cu, self.more = rows, cu_of(rows), dev(rows)
+        bf16 = dict(dtype=torch.bfloat16, device="cuda")
+        self.x = randn(gen(seed), m, self.d).bfloat16()
+        self.n8, self.ns = torch.empty(m, self.d, dtype=torch.int8, device="cuda"), torch.empty(m, device="cuda")
+        self.a8, self.as_ = torch.empty(m, qd, dtype=torch.int8, device="cuda"), torch.empty(m, device="cuda")
+        self.qkv, self.a, self.y = (torch.empty(m, w, **bf16) for w in (self.wide, qd, self.d))
+        need = S.surge_cache_attention_workspace(c.desc, max(rows), self.heads)
+        self.space = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+        return self
+
+    def run(self, stream):
+        c, d, m = self.c, self.d, sum(self.given)
+        wide, qd, kd = self.wide, self.heads * self.c.dh, self.c.hk * self.c.dh
+        c.lengths.add_(self.more)
+        S.surge_op_block_norm(m, d, S.NORM_RMS, self.x, d, None, 0, None, None, None, None, 0, 1.0, self.gamma,
+                              None, EPS, None, 0, None, 0, self.n8, d, self.ns, stream)
+        S.surge_op_linear_i8(m, wide, d, self.n8, d, self.ns, self.w["qkv"], self.ws["qkv"], self.bias["qkv"],
+                             None, 0, 0, self.qkv, wide, stream)
+        S.surge_op_cache_write(c.desc, m, self.cu, self.qkv[:, qd:], wide, self.qkv[:, qd + kd:], wide, stream)
+        S.surge_op_cache_attention(c.desc, m, self.cu, max(self.given), self.heads, True, c.dh ** -0.5, self.qkv,
+                                   wide, self.space, self.a, qd, stream)
+        S.surge_op_quantize_rows(m, qd, self.a, qd, self.a8, qd, self.as_, stream)
+        S.surge_op_linear_i8(m, d, qd, self.a8, qd, self.as_, self.w["o"], self.ws["o"], self.bias["o"], self.x, d,
+                             2, self.y, d, stream)
+
+    def check(self):
+        """Each operator against its definition of what the one before it gave."""
+        torch = torch_cuda()
+        c, qd, kd = self.c, self.heads * self.c.dh, self.c.hk * self.c.dh
+        p = dict(x=self.x, block=None, post_gamma=None, gate=None, gate_rows=None, pre_gamma=self.gamma, pre_beta=None)
+        check_i8(self.n8, self.ns, *norm_reference(p, False, 1.0, self.d)[2:], self.d)
+        layer = lambda x, xs, name: dict(x=x, xs=xs, w=self.w[name], ws=self.ws[name],  # noqa: E731
+                                         bias=self.bias[name], res=self.x)
+        within(self.qkv, *linear_reference({**layer(self.n8, self.ns, "qkv"), "res": self.qkv}, 0))
+        at = 0
+        for i, r in enumerate(self.given):
+            for w in range(2):
+                new = self.qkv[at:at + r, qd + w * kd:qd + (w + 1) * kd]
+                if r:
+                    c.held[i][w] = torch.cat([c.held[i][w], values(*quantized(new)).view(r, c.hk, c.dh)])
+            at += r
+        c.lengths_np = c.lengths_np + np.array(self.given)
+        assert np.array_equal(c.lengths.cpu().numpy(), c.lengths_np)
+        within(self.a, *reference(c, self.qkv[:, :qd].contiguous(), self.given, self.heads, True))
+        q, s = quantized32(self.a)
+        assert torch.equal(self.a8.cpu(), q) and torch.equal(self.as_.cpu(), s)
+        within(self.y, *linear_reference(layer(self.a8, self.as_, "o"), 2))
+
+
+BLOCKS = [([0, 40, 3, 0, 700], 384, 16, 6, 3, 64), ([2000, 0, 5000], 256, 64, 16, 4, 128), ([5, 90], 128, 32, 8, 8, 32)]
+
+
+@pytest.mark.parametrize("lengths,d,page,heads,hk,dh", BLOCKS)
+def test_block_of_a_decoder(lengths, d, page, heads, hk, dh):
+    """Prompts, then single tokens, then drafts, one sequence without any."""
+    torch = torch_cuda()
+    b, n = Block(lengths, d, page, heads, hk, dh, d), len(lengths)
+    for i, rows in enumerate(([70] + [130] * (n - 1), [1] * n, [5] * (n - 1) + [0])):
+        b.rows(rows, i).run(torch.cuda.current_stream())
+        b.check()
+
+
+def test_block_of_a_decoder_captured_and_replayed():
+    """Replayed as its answers grow, with eager work between: the eager block's bits."""
+    torch = torch_cuda()
+    eager, replayed = (Block(*BLOCKS[1], 3).rows([2, 1, 2], 1) for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        replayed.run(torch.cuda.current_stream())
+    for step in range(5):
+        eager.x.copy_(randn(gen(step), *eager.x.shape))
+        replayed.x.copy_(eager.x)
+        graph.replay()
+        eager.run(torch.cuda.current_stream())
+        if step % 2:
+            torch.cuda.synchronize()
+        assert torch.equal(eager.y, replayed.y) and torch.equal(eager.c.lengths, replayed.c.lengths)
+    assert eager.c.lengths.cpu().tolist() == [2010, 5, 5010]
+
+
+@pytest.mark.parametrize("heads,hk,dh", [(12, 12, 64), (8, 2, 128), (16, 4, 32)])
+def test_states_of_an_encoder_kept_in_4_bits(heads, hk, dh):
+    """Keys and values projected from texts' states by the library's layer, kept in
+    the cache, read by latent queries of each text without a mask."""
+    torch = torch_cuda()
+    texts, d, latents = [48, 3, 200, 64, 1, 130, 17], 384, 9
+    t, w = sum(texts), 2 * hk * dh
+    g = gen(heads)
+    x = randn(g, t, d).bfloat16()
+    wt, bias = (randn(g, w, d) / math.sqrt(d)).bfloat16(), 0.1 * randn(g, w)
+    kv = torch.empty(t, w, dtype=torch.bfloat16, device="cuda")
+    S.surge_op_linear(t, w, d, x, wt, bias, None, 0, kv)
+    ref = x.double() @ wt.double().t().contiguous() + bias.double()
+    size = x.double().abs() @ wt.double().abs().t().contiguous() + bias.double().abs()
+    within(kv, ref, BF16 * ref.abs() + 1.01 * (d + 2) * F32 * size)
+    c = Cache(texts, 32, hk, dh, 1)
+    S.surge_op_cache_write(c.desc, t, cu_of(texts), kv, w, kv[:, w // 2:], w, torch.cuda.current_stream())
+    ends = np.cumsum([0] + texts)
+    c.held = [[values(*quantized(y[a:b])).view(b - a, hk, dh) for y in (kv[:, :w // 2], kv[:, w // 2:])]
+              for a, b in zip(ends, ends[1:])]
+    check(c, [latents] * len(texts), heads, False, 2)
