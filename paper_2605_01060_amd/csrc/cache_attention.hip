@@ -20,24 +20,25 @@
 // operands), so K needs no LDS; V goes through it to be read transposed.  The next
 // block's codes are loaded while one is computed (two ahead changed nothing).  Bound
 // by memory where there is much of it: one query of 32 / 8 heads x 128 over 48 x about
-// 8,000 keys takes 82 us, 5.3 TB/s, over 100,003 keys 25 us, of which the first 4 find
+// 8,000 keys takes 84 us, 5.2 TB/s, over 100,003 keys 25 us, of which the first 4 find
 // the share and the first codes.  The VALU is half busy then, a half of it decoding.
 //
 // 64 or 128 rows a tile (prompts, many drafts): four waves decode blocks of 64 keys
 // into LDS together, a block ahead, and take 32x32x16 MFMAs from there; for 64 rows
 // two waves share 32 rows and halve the keys (64 x 16 queries x 3001 keys, 16 / 4 x
 // 128: 97 -> 61 us against waves with keys of their own).  8 x 2048 queries x 8192
-// keys, 16 x 128: 1,044 us, 1,053 TFLOP/s, 16 x 64 607 us, 905 TFLOP/s, 16 x 32 471
+// keys, 16 x 128: 1,059 us, 1,039 TFLOP/s, 16 x 64 620 us, 886 TFLOP/s, 16 x 32 476
 // us; what bounds it is the power limit and the VALU, as in cross attention.  Blocks
 // of 32 keys with three units a CU were 4 to 11 % slower here.
 //
 // Lengths are known on the device alone.  Where a unit (a tile of a sequence and key
 // head) has a long way to go and units are few, all units' blocks of keys are shared
 // out evenly to as many workgroups as the chip holds, each of which finds its share
-// from the lengths (2.3 us); a second kernel joins the parts of a unit that is cut.
-// 4 x about 1500 queries x about 6000 keys, 16 / 4 x 128: 402 us with a unit a
-// workgroup, 247 so.  Otherwise a unit is a workgroup's, or a wave's,
-// longest first.
+// from the lengths (2 to 3 us); a second kernel joins the parts of a unit that is cut.
+// 4 x about 1500 queries x about 6000 keys, 16 / 4 x 128: 384 us with a unit a
+// workgroup, 252 so.  Otherwise a unit is a workgroup's, or where it is short a wave's,
+// the last tiles of all sequences first; sequences are in their order, whatever their
+// lengths, so that one long one among many is waited for (cache_shape.h).
 #include <float.h>
 #include <math.h>
 
@@ -226,10 +227,10 @@ __device__ __forceinline__ int worker_of(int active) {
 // workers and the longest is within what a cut would save (`fit`), a whole unit.  The
 // parts of a unit that is cut are joined afterwards; who has the last one knows where
 // they started.  Measured, us, a unit a workgroup / equal shares / equal parts:
-//   16 x 5 queries x about 3001 keys, 16 / 4 x 128    40 / 24 / 20
-//   64 x 5 x about 3001, 16 / 4 x 128                 42 / 40 / 44
-//   48 x 1 x about 8000, 32 / 8 x 128                 112 / 87 / 100
-//   64 x 4 x 4000, 32 / 8 x 128                       53 / 70 / 58 (uncut, of which 3
+//   16 x 5 queries x about 3001 keys, 16 / 4 x 128    41 / 22 / 20
+//   64 x 5 x about 3001, 16 / 4 x 128                 42 / 39 / 46
+//   48 x 1 x about 8000, 32 / 8 x 128                 111 / 88 / 106
+//   64 x 4 x 4000, 32 / 8 x 128                       52 / 70 / 57 (uncut, of which 3
 //                                                     find the shares, 3 the join)
 template <class Fit, class Body>
 __device__ __forceinline__ void shared_units(const CacheAttention& a, Fit fit, Body body) {

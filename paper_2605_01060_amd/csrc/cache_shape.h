@@ -49,10 +49,10 @@ inline CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_
   const int64_t most = ((max_length - 1) >> s.block_shift) + 1;  // blocks of a unit
   // Sharing costs 2 us to find the shares and 5 us for the join, or 13 where tiles'
   // parts are 64 KiB each, a block 1 us (64 keys for a tile, 128 for few rows).  It is
-  // left where units are short or fill the chip twice over.  Measured, a unit a
-  // workgroup / shared, us:
+  // left where units are short, or of few rows are more than the chip holds, of tiles
+  // more than twice as many.  Measured, a unit a workgroup / shared, us:
   //   30 x 1 x 800, 16 / 4 x 128 10 / 12; 200 x 4 x 500, 12 x 64 23 / 45; 48 x 1 x about
-  //   8000, 32 / 8 x 128 96 / 87
+  //   8000, 32 / 8 x 128 111 / 88
   //   (few tiles) 10 x 12 x 1100, 32 / 8 x 128 23 / 18; 1 x 128 x 2000, 8 x 128 47 / 23
   //   (more) 34 x 148 x 1938, 12 x 64 61 / 77; 8 x 2048 x 8192, 16 x 128 1047 / 1144
   s.least_share = cls >= 2 ? 8 : 2;
@@ -62,9 +62,9 @@ inline CacheShape cache_attention_shape(int64_t n_seqs, int64_t max_rows, int n_
     s.workers = workers;
   // Where units of few rows are short, or very many and not long, a wave has one for
   // itself: no waves without keys and no join of four.  Measured, a workgroup / a wave, us:
-  // 400 x 1 x 60, 32 / 8 x 128 17.0 / 11.0; 200 x 8 x 100, 16 / 4 x 128 15.0 / 10.7; 1000 x 8 x
-  // 240, 32 / 8 x 128 109 / 88, 1000 x 8 x 1024 286 / 251, 800 x 1 x 1024 161 / 174; but 140 x 1
-  // x 240 12.5 / 14.1 and 400 x 1 x 900 79 / 90.  max_length says nothing of most sequences,
+  // 400 x 1 x 60, 32 / 8 x 128 17.0 / 11.2; 200 x 8 x 100, 16 / 4 x 128 15.0 / 10.5; 1000 x 8 x
+  // 240, 32 / 8 x 128 113 / 89, 1000 x 8 x 1024 286 / 254, 800 x 1 x 1024 162 / 173; but 140 x 1
+  // x 240 12.2 / 14.0 and 400 x 1 x 900 80 / 92.  max_length says nothing of most sequences,
   // but one may be as long, and the call then waits for its wave: among 800 x 1 of about 200
   // keys, 32 / 8 x 128, one of 1024 43 / 40, of 2048 43 / 66, of 30,000 212 / 773.
   s.wave_units = cls < 2 && s.workers == 0 && s.units > workers &&

@@ -12,8 +12,9 @@
 // bytes a lane, 128 or 256 of a row together, and writes the codes of
 // neighbouring tokens, which lie behind each other in a page, together too.  Bound
 // by memory, or in small calls by a chain of three loads (offsets, length, table):
-// 100,003 rows x 8 x 128 are written in 77 us, 6.7 TB/s, most of it read, and read
-// back in 103, 5.0 TB/s, most of it written; a copy moves 4.95.  64 rows take 4.7 us.
+// 100,003 rows x 8 x 128 are written in 77 us, 6.7 TB/s, most of it read (three sets of
+// 410 MB in turn, which no cache holds), and read back in 103, 5.0 TB/s, most of it
+// written; a copy, half of each, moves 4.9.  64 rows take 4.7 us.
 // Rows are loaded and stored past the caches (nontemporal), places found once for
 // four heads and neighbouring rows kept on one XCD: 192,000 rows x 12 x 64, written
 // and read, 383 us without them, 256 with.
