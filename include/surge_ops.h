@@ -292,8 +292,8 @@ surge_status surge_op_cross_attention(const surge_cross_plan* plan, const uint16
  * max_length and n_rows at most 2^30.  The struct is read by the call.  A call that
  * needs a larger grid than a launch has is refused with SURGE_ERR_CAPACITY: a write or
  * read of more than 2^29 rows, counted for each four key heads, attention of more than
- * 2^23 units, a unit being 128 rows (query x heads of the group; 16, 32 or 64 where a
- * sequence has no more) of a sequence and key head.
+ * 2^23 units, a unit being 128 of a sequence's max_rows rows (each one of the query
+ * heads that share a key head; 16, 32 or 64 where there are no more).
  */
 typedef struct surge_kv_cache {
   uint8_t* d_pages;
